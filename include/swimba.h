@@ -398,6 +398,105 @@ swimba_status swimba_router_linear(int64_t tokens, int32_t d_model, int32_t nexp
                                    const void *u, const void *W_g, void *router_logits, void *hip_stream);
 
 /*
+ * Layer norm of token features, the step in front of the router's and the projections' linear maps:
+ *   r_t = x_t + residual_t, rounded to res_dtype (the residual stream as it is stored);  x_t itself where residual is NULL
+ *   m_t = mean_d r_t[d],  s_t = 1 / sqrt(mean_d (r_t[d] - m_t)^2 + eps),   u_t[d] = (r_t[d] - m_t) s_t gamma[d] + beta[d]
+ *   x        (tokens, d_model) io          residual (tokens, d_model) res_dtype [in]  NULL = none
+ *   gamma, beta (d_model) fp32 [in]        NULL = 1, 0
+ *   u        (tokens, d_model) io  [out]
+ *   sum      (tokens, d_model) res_dtype [out] r, where residual is given; NULL = not wanted.  May be the buffer of
+ *            residual or (of one type) of x: every element is read, then written, by one lane.
+ *   mean, rstd (tokens) fp32 [out]         m and s, what the backward pass needs; NULL = not wanted
+ * res_dtype is io_dtype, or SWIMBA_F32 for a residual stream kept in fp32 beside bf16 features; without a residual it has
+ * to be io_dtype.  eps > 0 and finite.  The mean and the centred squares are summed in fp32 in two passes over the row in
+ * registers, so an offset that is large beside the deviations costs what storing the row costs and no more.  A row that is
+ * not finite reaches nothing but its own outputs.  d_model up to SWIMBA_MAX_DMODEL_GENERIC.  Large tensors
+ * 16-byte aligned, gamma, beta, mean and rstd by element; rows need no alignment of their own.  No workspace, one launch.
+ */
+swimba_status swimba_layer_norm(int64_t tokens, int32_t d_model, int32_t io_dtype, int32_t res_dtype, const void *x,
+                                const void *residual, const float *gamma, const float *beta, float eps, void *u, void *sum,
+                                float *mean, float *rstd, void *hip_stream);
+
+/*
+ * Its backward pass.  With xh = (r - m) s and g = du gamma:
+ *   dx = s (g - mean_d g - xh mean_d(g xh)) + d_sum,   dgamma = sum_t du_t xh_t,   dbeta = sum_t du_t
+ *   du       (tokens, d_model) io [in]     gradient of u
+ *   r        (tokens, d_model) res_dtype [in]   the rows that were normalised (x, or sum where there was a residual)
+ *   mean, rstd (tokens) fp32 [in]          as the forward stored them
+ *   d_sum    (tokens, d_model) res_dtype [in]   gradient that reaches r by itself, along the residual stream; NULL = none
+ *   dx       (tokens, d_model) res_dtype [out]  gradient of r, so of x and of residual; may be the buffer of d_sum
+ *   dx_io    (tokens, d_model) io [out]    the same, rounded to the type of x where that is not res_dtype; NULL = not
+ *            wanted, and refused where the types are equal (dx is it)
+ *   dgamma, dbeta (d_model) fp32 [out]     NULL = not wanted
+ * The sums over the tokens are taken in fp32 in an order that sizes alone decide (zero for no tokens).
+ *   workspace >= swimba_layer_norm_bwd_workspace_bytes(tokens, d_model), 256-byte aligned.
+ */
+size_t swimba_layer_norm_bwd_workspace_bytes(int64_t tokens, int32_t d_model);
+swimba_status swimba_layer_norm_bwd(int64_t tokens, int32_t d_model, int32_t io_dtype, int32_t res_dtype, const void *du,
+                                    const void *r, const float *gamma, const float *mean, const float *rstd,
+                                    const void *d_sum, void *dx, void *dx_io, float *dgamma, float *dbeta, void *workspace,
+                                    size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Routing with per-expert counts and a balance loss, for training the router.  The tokens come in `groups` groups of
+ * `tokens` each (the sequences of a batch, or one group of all tokens); every group has a loss of its own over the n of
+ * its tokens that count:
+ *   pi_t = softmax(logits_t) over all E, K_t its top_k as swimba_router_topk picks them
+ *   counts[e] = #{t : e in K_t},   prob_mean[e] = (1/n) sum_t pi_t[e],   loss = E sum_e counts[e] / (k n) prob_mean[e]
+ * (1 for an even load, up to E / k where the same experts take every token; 0 where n = 0).
+ *   logits   (groups, tokens, E) io [in]
+ *   mask     (groups, tokens) uint8 [in]  0: the token does not count (padding); NULL: all count.  Its logits reach
+ *            nothing but its own topk_idx and topk_w, whatever they hold.  A token whose logits are all -inf does not count either.
+ *   topk_idx, topk_w (groups, tokens, k) [out]  of every token: the experts of swimba_router_topk and, to the rounding of the sum
+ *            over the experts, its weights;
+ *            NULL = not wanted
+ *   counts   (groups, E) int32 [out]    prob_mean (groups, E) fp32 [out]  NULL = not wanted    loss (groups) fp32 [out]
+ * A logit that is NaN or +inf in a token that counts makes the probabilities and the loss of its group NaN.
+ * At most 2^31 - 1 tokens to a group and 2^38 in all.  Element-aligned pointers; rows of logits that start 16-byte
+ * aligned (by pointer and E) are read in larger pieces.
+ *   workspace >= swimba_router_balance_workspace_bytes(groups, tokens, nexperts), 256-byte aligned.
+ */
+size_t swimba_router_balance_workspace_bytes(int64_t groups, int64_t tokens, int32_t nexperts);
+swimba_status swimba_router_balance(int64_t groups, int64_t tokens, int32_t nexperts, int32_t top_k, int32_t io_dtype,
+                                    const void *logits, const uint8_t *mask, int32_t *topk_idx, float *topk_w,
+                                    int32_t *counts, float *prob_mean, float *loss, void *workspace, size_t workspace_bytes,
+                                    void *hip_stream);
+
+/*
+ * The gradient of the logits, from the routing weights and from the balance loss, whose counts are held constant:
+ *   g_t[e] = [e = topk_idx_t[r]] d_topk_w_t[r]  +  [t counts] d_loss (E / n) counts[e] / (k n),    n = sum_e counts[e] / k
+ *   d_logits_t = pi_t (g_t - sum_e pi_t[e] g_t[e])
+ *   logits, mask as above              topk_idx (groups, tokens, k) int32 [in]
+ *   d_topk_w (groups, tokens, k) fp32 [in]  gradient of the routing weights, of every token whether it counts or not;
+ *            NULL = zero (topk_idx is not read then and may be NULL)
+ *   counts   (groups, E) int32, d_loss (groups) fp32 [in]  both NULL: no balance loss.  Counts that were summed over the
+ *            ranks of a data-parallel run give each rank its part of the gradient of the loss over all of them.
+ *   d_logits (groups, tokens, E) io [out]
+ * Indices outside [0, E) are passed over.  A token that does not count and whose d_topk_w are all zero (or NULL), and one
+ * whose logits are all -inf, get zeros whatever their logits hold.  No workspace, one launch.
+ */
+swimba_status swimba_router_bwd(int64_t groups, int64_t tokens, int32_t nexperts, int32_t top_k, int32_t io_dtype,
+                                const void *logits, const uint8_t *mask, const int32_t *topk_idx, const float *d_topk_w,
+                                const int32_t *counts, const float *d_loss, void *d_logits, void *hip_stream);
+
+/*
+ * Backward pass of swimba_router_linear:
+ *   du_t[d] = sum_e d_logits_t[e] W_g[e][d] + du_add_t[d],    dW_g[e][d] = sum_t d_logits_t[e] u_t[d]
+ *   u (tokens, d_model) io, W_g (E, d_model) io, d_logits (tokens, E) io [in]
+ *   du_add   (tokens, d_model) io [in]   gradient that reaches u by other ways (the projections); NULL = none
+ *   du       (tokens, d_model) io [out]  NULL = not wanted; may be the buffer of du_add
+ *   dW_g     (E, d_model) fp32 [out]     NULL = not wanted
+ * fp32 accumulation; du is rounded once, dW_g is not rounded, its sum over the tokens is taken in an order that sizes alone decide.
+ * u is read for dW_g only, W_g for du only; the other may be NULL.  Limits, alignment (du, du_add as u) and the
+ * element-wise reading of rows that are no multiple of 16 bytes as in swimba_router_linear; dW_g by element.
+ *   workspace >= swimba_router_linear_bwd_workspace_bytes(tokens, d_model, nexperts), 256-byte aligned.
+ */
+size_t swimba_router_linear_bwd_workspace_bytes(int64_t tokens, int32_t d_model, int32_t nexperts);
+swimba_status swimba_router_linear_bwd(int64_t tokens, int32_t d_model, int32_t nexperts, int32_t io_dtype, const void *u,
+                                       const void *W_g, const void *d_logits, const void *du_add, void *du, float *dW_g,
+                                       void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Routed expert in-projection, the step upstream of the mixer (paper, MoE-parameterized
  * SSM: the expert streams are expert-specific linear projections of the token features;
  * only the active set K_t enters the mix).  For every token t and every e in K_t:

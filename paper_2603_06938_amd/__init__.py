@@ -13,6 +13,9 @@ _BINDING_NAMES = (
     "PATH_CHAIN_BF16", "PATH_CHAIN_F32", "swimba_step_static",
     "PATH_GENERIC", "PATH_STAGED", "PATH_SINGLE_PASS",
     "swimba_probe_copy", "swimba_probe_mfma", "alloc_workspace", "workspace_views", "dims_of",
+    "swimba_layer_norm", "swimba_layer_norm_bwd", "swimba_layer_norm_bwd_workspace_bytes", "swimba_router_balance",
+    "swimba_router_balance_workspace_bytes", "swimba_router_bwd", "swimba_router_linear_bwd",
+    "swimba_router_linear_bwd_workspace_bytes",
     "make_dims", "SwimbaError", "library_loaded",
 )
 

@@ -149,6 +149,23 @@ def _load():
         lib.swimba_step.argtypes = [dp] + [vp] * 11 + [vp, sz, vp]
         lib.swimba_step_static.restype = i32
         lib.swimba_step_static.argtypes = [dp] + [vp] * 11 + [vp]
+        f32 = ctypes.c_float
+        lib.swimba_layer_norm.restype = i32
+        lib.swimba_layer_norm.argtypes = [i64, i32, i32, i32] + [vp] * 4 + [f32] + [vp] * 5
+        lib.swimba_layer_norm_bwd_workspace_bytes.restype = sz
+        lib.swimba_layer_norm_bwd_workspace_bytes.argtypes = [i64, i32]
+        lib.swimba_layer_norm_bwd.restype = i32
+        lib.swimba_layer_norm_bwd.argtypes = [i64, i32, i32, i32] + [vp] * 10 + [vp, sz, vp]
+        lib.swimba_router_balance_workspace_bytes.restype = sz
+        lib.swimba_router_balance_workspace_bytes.argtypes = [i64, i64, i32]
+        lib.swimba_router_balance.restype = i32
+        lib.swimba_router_balance.argtypes = [i64, i64, i32, i32, i32] + [vp] * 7 + [vp, sz, vp]
+        lib.swimba_router_bwd.restype = i32
+        lib.swimba_router_bwd.argtypes = [i64, i64, i32, i32, i32] + [vp] * 8
+        lib.swimba_router_linear_bwd_workspace_bytes.restype = sz
+        lib.swimba_router_linear_bwd_workspace_bytes.argtypes = [i64, i32, i32]
+        lib.swimba_router_linear_bwd.restype = i32
+        lib.swimba_router_linear_bwd.argtypes = [i64, i32, i32, i32] + [vp] * 6 + [vp, sz, vp]
         lib.swimba_probe_copy.restype = i32
         lib.swimba_probe_copy.argtypes = [vp, vp, sz, vp]
         lib.swimba_probe_mfma.restype = i32
@@ -171,6 +188,7 @@ def _load_native():
                 "_native.so is not built (%s); run `python -c 'import __graft_entry__ as g; g.build()'`" % NATIVE_PATH)
         from . import _native as module
         module.classes(MixerOut, StepOut, SwimbaError)
+        module.training_classes(NormOut, NormGrad, BalanceOut, LinearGrad)
         _native = module
     return _native
 
@@ -279,6 +297,88 @@ def swimba_mixer_fwd(x, dt, A, D, B_experts, C_experts, router_logits, top_k: in
 def swimba_router_linear(u, W_g, router_logits=None) -> torch.Tensor:
     """u (..., Dm), W_g (E, Dm) -> routing logits (..., E) in the io dtype."""
     return (_native or _load_native()).router_linear(u, W_g, router_logits)
+
+
+# ---- training the routing --------------------------------------------------------------
+
+class NormOut(NamedTuple):
+    u: torch.Tensor
+    sum: Optional[torch.Tensor]
+    mean: Optional[torch.Tensor]
+    rstd: Optional[torch.Tensor]
+
+
+class NormGrad(NamedTuple):
+    dx: torch.Tensor
+    dx_io: Optional[torch.Tensor]
+    dgamma: Optional[torch.Tensor]
+    dbeta: Optional[torch.Tensor]
+
+
+class BalanceOut(NamedTuple):
+    loss: torch.Tensor
+    counts: torch.Tensor
+    prob_mean: torch.Tensor
+    topk_idx: Optional[torch.Tensor]
+    topk_w: Optional[torch.Tensor]
+
+
+class LinearGrad(NamedTuple):
+    du: Optional[torch.Tensor]
+    dW_g: Optional[torch.Tensor]
+
+
+def swimba_layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, residual=None, *, u=None, sum=None, mean=None, rstd=None,
+                      want_sum: bool = True, want_stats: bool = False) -> NormOut:
+    """Layer norm over the last axis of x (..., Dm), of x + residual where that is given (x's dtype, or float32 beside
+    bfloat16).  `sum` is the stored x + residual (pass sum=residual to update the stream in place); mean and rstd (...) fp32,
+    on want_stats, are what swimba_layer_norm_bwd takes."""
+    return (_native or _load_native()).layer_norm(x, gamma, beta, eps, residual, u, sum, mean, rstd, want_sum, want_stats)
+
+
+def swimba_layer_norm_bwd_workspace_bytes(tokens: int, d_model: int) -> int:
+    return int(_load().swimba_layer_norm_bwd_workspace_bytes(tokens, d_model))
+
+
+def swimba_layer_norm_bwd(du, r, gamma, mean, rstd, d_sum=None, *, dx=None, dx_io=None, dgamma=None, dbeta=None, workspace=None,
+                          want_dx_io: bool = True, want_weights: bool = True) -> NormGrad:
+    """Gradients of swimba_layer_norm.  du (..., Dm): gradient of u; r: the normalised rows (x, or `sum` where there was a
+    residual); d_sum: gradient that reaches r along the residual stream.  dx has r's dtype (pass dx=d_sum to work in place);
+    where that is not du's, dx_io holds the same values in du's."""
+    return (_native or _load_native()).layer_norm_bwd(du, r, gamma, mean, rstd, d_sum, dx, dx_io, dgamma, dbeta, workspace,
+                                                      want_dx_io, want_weights)
+
+
+def swimba_router_balance_workspace_bytes(groups: int, tokens: int, nexperts: int) -> int:
+    return int(_load().swimba_router_balance_workspace_bytes(groups, tokens, nexperts))
+
+
+def swimba_router_balance(router_logits, top_k: int, mask=None, *, per_sequence: bool = False, loss=None, counts=None,
+                          prob_mean=None, topk_idx=None, topk_w=None, workspace=None, want_topk: bool = True) -> BalanceOut:
+    """Routing of router_logits (..., E) with per-expert counts and the balance loss, of all tokens together or, with
+    per_sequence, of each entry of the first axis by itself.  mask (...) bool or uint8: the tokens that count.
+    loss (S), counts (S, E) int32, prob_mean (S, E) with S = 1 or the first axis; topk_idx, topk_w (..., top_k)."""
+    return (_native or _load_native()).router_balance(router_logits, top_k, mask, per_sequence, loss, counts, prob_mean, topk_idx,
+                                                      topk_w, workspace, want_topk)
+
+
+def swimba_router_bwd(router_logits, topk_idx=None, d_topk_w=None, counts=None, d_loss=None, mask=None, *,
+                      top_k: Optional[int] = None, d_logits=None) -> torch.Tensor:
+    """Gradient of router_logits (..., E) from that of the routing weights, d_topk_w (..., k) at topk_idx, and that of the
+    balance loss, d_loss (S) with the counts (S, E) and the mask of swimba_router_balance; either may be left out.
+    top_k is needed where there are counts and no topk_idx."""
+    return (_native or _load_native()).router_bwd(router_logits, topk_idx, d_topk_w, counts, d_loss, mask, d_logits, top_k)
+
+
+def swimba_router_linear_bwd_workspace_bytes(tokens: int, d_model: int, nexperts: int) -> int:
+    return int(_load().swimba_router_linear_bwd_workspace_bytes(tokens, d_model, nexperts))
+
+
+def swimba_router_linear_bwd(u, W_g, d_logits, du_add=None, *, du=None, dW_g=None, workspace=None, want_du: bool = True,
+                             want_dW_g: bool = True) -> LinearGrad:
+    """Gradients of swimba_router_linear: du (..., Dm) in the io dtype, with du_add (the gradient that reaches u by other
+    ways) added before it is rounded, and dW_g (E, Dm) in fp32."""
+    return (_native or _load_native()).router_linear_bwd(u, W_g, d_logits, du_add, du, dW_g, workspace, want_du, want_dW_g)
 
 
 def swimba_expert_proj_workspace_bytes(dims: swimba_dims, d_model: int) -> int:

@@ -334,6 +334,146 @@ swimba_status swimba_router_linear(int64_t tokens, int32_t d_model, int32_t nexp
                                 (hipStream_t)hip_stream);
 }
 
+// ---- what trains the routing --------------------------------------------------------------
+static swimba_status check_norm(int64_t tokens, int32_t d_model)
+{
+    if (tokens < 0 || d_model < 1) return SWIMBA_ERR_SHAPE;
+    if (d_model > SWIMBA_MAX_DMODEL_GENERIC || tokens > (1ll << 38)) return SWIMBA_ERR_UNSUPPORTED;
+    return SWIMBA_OK;
+}
+static swimba_status check_norm_types(int32_t io_dtype, int32_t res_dtype)
+{
+    if (io_dtype != SWIMBA_F32 && io_dtype != SWIMBA_BF16) return SWIMBA_ERR_DTYPE;
+    return res_dtype == io_dtype || res_dtype == SWIMBA_F32 ? SWIMBA_OK : SWIMBA_ERR_DTYPE;
+}
+
+swimba_status swimba_layer_norm(int64_t tokens, int32_t d_model, int32_t io_dtype, int32_t res_dtype, const void *x,
+                                const void *residual, const float *gamma, const float *beta, float eps, void *u, void *sum,
+                                float *mean, float *rstd, void *hip_stream)
+{
+    swimba_status st = check_norm_types(io_dtype, res_dtype);
+    if (st != SWIMBA_OK) return st;
+    if (!residual && res_dtype != io_dtype) return SWIMBA_ERR_DTYPE;
+    st = check_norm(tokens, d_model);
+    if (st != SWIMBA_OK) return st;
+    if (!(eps > 0.f) || eps > 3.4e38f) return SWIMBA_ERR_SHAPE;
+    if (tokens == 0) return SWIMBA_OK;
+    if (!x || !u || (sum && !residual)) return SWIMBA_ERR_NULL;
+    if (check_align(io_dtype, {x, residual, u, sum}, {}, {gamma, beta, mean, rstd}) != SWIMBA_OK) return SWIMBA_ERR_ALIGNMENT;
+    return launch_layer_norm(tokens, d_model, io_dtype, res_dtype, x, residual, gamma, beta, eps, u, sum, mean, rstd,
+                             (hipStream_t)hip_stream);
+}
+
+size_t swimba_layer_norm_bwd_workspace_bytes(int64_t tokens, int32_t d_model)
+{
+    if (check_norm(tokens, d_model) != SWIMBA_OK) return 0;
+    const size_t n = layer_norm_bwd_bytes(tokens, d_model);
+    return align_up(n > 0 ? n : 1, 256);
+}
+
+swimba_status swimba_layer_norm_bwd(int64_t tokens, int32_t d_model, int32_t io_dtype, int32_t res_dtype, const void *du,
+                                    const void *r, const float *gamma, const float *mean, const float *rstd,
+                                    const void *d_sum, void *dx, void *dx_io, float *dgamma, float *dbeta, void *workspace,
+                                    size_t workspace_bytes, void *hip_stream)
+{
+    swimba_status st = check_norm_types(io_dtype, res_dtype);
+    if (st != SWIMBA_OK) return st;
+    if (dx_io && res_dtype == io_dtype) return SWIMBA_ERR_DTYPE;
+    st = check_norm(tokens, d_model);
+    if (st != SWIMBA_OK) return st;
+    if (!workspace || workspace_bytes < swimba_layer_norm_bwd_workspace_bytes(tokens, d_model) || ((uintptr_t)workspace & 255u))
+        return SWIMBA_ERR_WORKSPACE;
+    if (tokens > 0 && (!du || !r || !mean || !rstd || !dx)) return SWIMBA_ERR_NULL;
+    if (check_align(io_dtype, {du, r, d_sum, dx, dx_io}, {}, {gamma, mean, rstd, dgamma, dbeta}) != SWIMBA_OK)
+        return SWIMBA_ERR_ALIGNMENT;
+    return launch_layer_norm_bwd(tokens, d_model, io_dtype, res_dtype, du, r, gamma, mean, rstd, d_sum, dx, dx_io, dgamma, dbeta,
+                                 (float *)workspace, (hipStream_t)hip_stream);
+}
+
+// Groups of tokens: each has counts of 31 bits; the launches have a block or more for every group.
+static swimba_status check_groups(int64_t groups, int64_t tokens, int32_t nexperts)
+{
+    if (groups < 0 || tokens < 0 || nexperts < 1) return SWIMBA_ERR_SHAPE;
+    if (nexperts > SWIMBA_MAX_EXPERTS || groups > (1 << 20) || tokens > INT32_MAX || groups * tokens > (1ll << 38))
+        return SWIMBA_ERR_UNSUPPORTED;
+    return SWIMBA_OK;
+}
+static swimba_status check_routing(int64_t groups, int64_t tokens, int32_t nexperts, int32_t top_k, int32_t io_dtype)
+{
+    if (io_dtype != SWIMBA_F32 && io_dtype != SWIMBA_BF16) return SWIMBA_ERR_DTYPE;
+    if (top_k < 1 || top_k > nexperts) return SWIMBA_ERR_SHAPE;
+    if (top_k > SWIMBA_MAX_TOPK) return SWIMBA_ERR_UNSUPPORTED;
+    return check_groups(groups, tokens, nexperts);
+}
+
+size_t swimba_router_balance_workspace_bytes(int64_t groups, int64_t tokens, int32_t nexperts)
+{
+    if (check_groups(groups, tokens, nexperts) != SWIMBA_OK) return 0;
+    const size_t n = balance_bytes(groups, tokens, nexperts);
+    return align_up(n > 0 ? n : 1, 256);
+}
+
+swimba_status swimba_router_balance(int64_t groups, int64_t tokens, int32_t nexperts, int32_t top_k, int32_t io_dtype,
+                                    const void *logits, const uint8_t *mask, int32_t *topk_idx, float *topk_w,
+                                    int32_t *counts, float *prob_mean, float *loss, void *workspace, size_t workspace_bytes,
+                                    void *hip_stream)
+{
+    swimba_status st = check_routing(groups, tokens, nexperts, top_k, io_dtype);
+    if (st != SWIMBA_OK) return st;
+    if (groups == 0) return SWIMBA_OK;
+    if (!workspace || workspace_bytes < swimba_router_balance_workspace_bytes(groups, tokens, nexperts) ||
+        ((uintptr_t)workspace & 255u))
+        return SWIMBA_ERR_WORKSPACE;
+    if ((tokens > 0 && !logits) || !counts || !loss) return SWIMBA_ERR_NULL;
+    if (check_align(io_dtype, {}, {logits}, {topk_idx, topk_w, counts, prob_mean, loss}) != SWIMBA_OK) return SWIMBA_ERR_ALIGNMENT;
+    return launch_router_balance(groups, tokens, nexperts, top_k, io_dtype, logits, mask, topk_idx, topk_w, counts, prob_mean,
+                                 loss, workspace, (hipStream_t)hip_stream);
+}
+
+swimba_status swimba_router_bwd(int64_t groups, int64_t tokens, int32_t nexperts, int32_t top_k, int32_t io_dtype,
+                                const void *logits, const uint8_t *mask, const int32_t *topk_idx, const float *d_topk_w,
+                                const int32_t *counts, const float *d_loss, void *d_logits, void *hip_stream)
+{
+    swimba_status st = check_routing(groups, tokens, nexperts, top_k, io_dtype);
+    if (st != SWIMBA_OK) return st;
+    if (groups == 0 || tokens == 0) return SWIMBA_OK;
+    if (!logits || !d_logits || (d_topk_w && !topk_idx) || !counts != !d_loss) return SWIMBA_ERR_NULL;
+    if (check_align(io_dtype, {}, {logits, d_logits}, {topk_idx, d_topk_w, counts, d_loss}) != SWIMBA_OK)
+        return SWIMBA_ERR_ALIGNMENT;
+    return launch_router_bwd(groups, tokens, nexperts, top_k, io_dtype, logits, mask, topk_idx, d_topk_w, counts, d_loss, d_logits,
+                             (hipStream_t)hip_stream);
+}
+
+static swimba_status check_linear(int64_t tokens, int32_t d_model, int32_t nexperts)
+{
+    if (tokens < 0 || d_model < 1 || nexperts < 1) return SWIMBA_ERR_SHAPE;
+    if (nexperts > SWIMBA_MAX_EXPERTS || d_model > 65536 || tokens > (1ll << 38)) return SWIMBA_ERR_UNSUPPORTED;
+    return SWIMBA_OK;
+}
+
+size_t swimba_router_linear_bwd_workspace_bytes(int64_t tokens, int32_t d_model, int32_t nexperts)
+{
+    if (check_linear(tokens, d_model, nexperts) != SWIMBA_OK) return 0;
+    const size_t n = router_linear_bwd_bytes(tokens, d_model, nexperts);
+    return align_up(n > 0 ? n : 1, 256);
+}
+
+swimba_status swimba_router_linear_bwd(int64_t tokens, int32_t d_model, int32_t nexperts, int32_t io_dtype, const void *u,
+                                       const void *W_g, const void *d_logits, const void *du_add, void *du, float *dW_g,
+                                       void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (io_dtype != SWIMBA_F32 && io_dtype != SWIMBA_BF16) return SWIMBA_ERR_DTYPE;
+    swimba_status st = check_linear(tokens, d_model, nexperts);
+    if (st != SWIMBA_OK) return st;
+    if (!workspace || workspace_bytes < swimba_router_linear_bwd_workspace_bytes(tokens, d_model, nexperts) ||
+        ((uintptr_t)workspace & 255u))
+        return SWIMBA_ERR_WORKSPACE;
+    if (tokens > 0 && (!d_logits || (du && !W_g) || (dW_g && !u) || (du_add && !du))) return SWIMBA_ERR_NULL;
+    if (check_align(io_dtype, {u, W_g, du_add, du}, {d_logits}, {dW_g}) != SWIMBA_OK) return SWIMBA_ERR_ALIGNMENT;
+    return launch_router_linear_bwd(tokens, d_model, nexperts, io_dtype, u, W_g, d_logits, du_add, du, dW_g, workspace,
+                                    (hipStream_t)hip_stream);
+}
+
 swimba_status swimba_stage_router(const swimba_dims *dims, const void *router_logits,
                                   void *workspace, size_t workspace_bytes, void *hip_stream)
 {

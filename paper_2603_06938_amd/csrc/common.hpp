@@ -72,6 +72,25 @@ swimba_status launch_router(int64_t tokens, int E, int K, int io_dtype, const vo
                             int32_t *idx, float *w, hipStream_t st);
 swimba_status launch_router_linear(int64_t tokens, int Dm, int E, int io_dtype, const void *u, const void *Wg,
                                    void *logits, hipStream_t st);
+// layer norm and its backward pass (layer_norm.hip)
+swimba_status launch_layer_norm(int64_t tokens, int D, int io_dtype, int res_dtype, const void *x, const void *residual,
+                                const float *gamma, const float *beta, float eps, void *u, void *sum, float *mean, float *rstd,
+                                hipStream_t st);
+size_t layer_norm_bwd_bytes(int64_t tokens, int D);
+swimba_status launch_layer_norm_bwd(int64_t tokens, int D, int io_dtype, int res_dtype, const void *du, const void *r,
+                                    const float *gamma, const float *mean, const float *rstd, const void *d_sum, void *dx,
+                                    void *dx_io, float *dgamma, float *dbeta, float *part, hipStream_t st);
+// training the router (router_train.hip)
+size_t balance_bytes(int64_t groups, int64_t tokens, int E);
+swimba_status launch_router_balance(int64_t groups, int64_t tokens, int E, int K, int io_dtype, const void *logits,
+                                    const uint8_t *mask, int32_t *topk_idx, float *topk_w, int32_t *counts, float *prob_mean,
+                                    float *loss, void *part, hipStream_t st);
+swimba_status launch_router_bwd(int64_t groups, int64_t tokens, int E, int K, int io_dtype, const void *logits, const uint8_t *mask,
+                                const int32_t *topk_idx, const float *d_topk_w, const int32_t *counts, const float *d_loss,
+                                void *d_logits, hipStream_t st);
+size_t router_linear_bwd_bytes(int64_t tokens, int D, int E);
+swimba_status launch_router_linear_bwd(int64_t tokens, int D, int E, int io_dtype, const void *u, const void *Wg, const void *dl,
+                                       const void *du_add, void *du, float *dW, void *part, hipStream_t st);
 swimba_status launch_cumsum(const Shape &s, int io_dtype, const void *dt, const float *A, float *cs,
                             hipStream_t st);
 swimba_status launch_state_scan(const Shape &s, const float *h0, float *h_final, float *states,

@@ -6,7 +6,10 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
+
+#include <limits>
 
 #include "swimba.h"
 #include "unlocked.hpp"
@@ -360,6 +363,251 @@ PyObject *step(PyObject *const *a)
     return named(g_step_out, {&y, &state, &idx});
 }
 
+// ---- what trains the routing: the calls run on their tensors' device, on the stream that is current there ----------------
+
+PyObject *g_norm_out = nullptr, *g_norm_grad = nullptr, *g_balance_out = nullptr, *g_linear_grad = nullptr;
+
+using Sizes = c10::SmallVector<int64_t, 6>;
+
+int32_t integer32(PyObject *o, const char *name)
+{
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Raised{};
+    if (v < std::numeric_limits<int32_t>::min() || v > std::numeric_limits<int32_t>::max())
+        raise(PyExc_ValueError, "%s is out of range", name);
+    return (int32_t)v;
+}
+
+int32_t size32(int64_t v, const char *name)
+{
+    if (v > std::numeric_limits<int32_t>::max()) raise(PyExc_ValueError, "%s is out of range", name);
+    return (int32_t)v;
+}
+
+void same_device(PyObject *o, const char *name, at::Device dev)
+{
+    if (o != Py_None && THPVariable_Unpack(o).device() != dev)
+        raise(PyExc_ValueError, "%s must be on %s, as the other tensors are", name, dev.str().c_str());
+}
+
+void *ptr_on(at::Device dev, PyObject *o, const char *name, at::ScalarType dtype, c10::IntArrayRef shape)
+{
+    void *p = ptr(o, name, dtype, shape);
+    same_device(o, name, dev);
+    return p;
+}
+
+void take_on(Out &out, PyObject *given, bool wanted, const char *name, at::ScalarType dtype, c10::IntArrayRef shape, at::Device dev)
+{
+    out.take(given, wanted, name, dtype, shape, dev);
+    same_device(out.obj, name, dev);
+}
+
+Workspace workspace_on(PyObject *given, size_t want, at::Device dev)
+{
+    Workspace ws(given, want, dev);
+    same_device(given, "workspace", dev);
+    return ws;
+}
+
+// leading sizes of a tensor of rows, and how many rows that is
+Sizes leading(const at::Tensor &t, int64_t *rows)
+{
+    Sizes s(t.sizes().begin(), t.sizes().end() - 1);
+    *rows = 1;
+    for (const int64_t n : s) *rows *= n;
+    return s;
+}
+
+// x gamma beta eps residual u sum mean rstd want_sum want_stats
+PyObject *layer_norm(PyObject *const *a)
+{
+    const at::Tensor &x = tensor(a[0], "x");
+    if (x.dim() < 1) raise(PyExc_ValueError, "x must have at least one dimension");
+    const at::ScalarType io = x.scalar_type(), f32 = at::kFloat;
+    const int32_t code = io_code(x);
+    const at::Device dev = gpu_of(x, "x");
+    const c10::DeviceGuard guard(dev);
+    const bool has = a[4] != Py_None;
+    const at::ScalarType res = has ? tensor(a[4], "residual").scalar_type() : io;
+    if (res != io && res != f32)
+        raise(PyExc_TypeError, "residual must have dtype %s or Float, got %s", c10::toString(io), c10::toString(res));
+    int64_t tokens;
+    const int64_t D = x.size(-1);
+    const Sizes lead = leading(x, &tokens);
+    const double eps = PyFloat_AsDouble(a[3]);
+    if (eps == -1. && PyErr_Occurred()) throw Raised{};
+    void *px = ptr(a[0], "x", io, x.sizes()), *pr = ptr_on(dev, a[4], "residual", res, x.sizes());
+    void *pg = ptr_on(dev, a[1], "gamma", f32, {D}), *pb = ptr_on(dev, a[2], "beta", f32, {D});
+    if (!has && a[6] != Py_None) raise(PyExc_ValueError, "sum is written only where there is a residual");
+    Out u, sum, mean, rstd;
+    const bool stats = truth(a[10]);
+    take_on(u, a[5], true, "u", io, x.sizes(), dev);
+    take_on(sum, a[6], has && truth(a[9]), "sum", res, x.sizes(), dev);
+    take_on(mean, a[7], stats, "mean", f32, lead, dev);
+    take_on(rstd, a[8], stats, "rstd", f32, lead, dev);
+    void *const hs = stream();
+    const int32_t Dm = size32(D, "d_model");
+    check(unlocked([&] {
+              return swimba_layer_norm(tokens, Dm, code, res == f32 ? SWIMBA_F32 : SWIMBA_BF16, px, pr, (float *)pg, (float *)pb,
+                                       (float)eps, u.data, sum.data, (float *)mean.data, (float *)rstd.data, hs);
+          }), "swimba_layer_norm");
+    return named(g_norm_out, {&u, &sum, &mean, &rstd});
+}
+
+// du r gamma mean rstd d_sum dx dx_io dgamma dbeta workspace want_dx_io want_weights
+PyObject *layer_norm_bwd(PyObject *const *a)
+{
+    const at::Tensor &du = tensor(a[0], "du"), &r = tensor(a[1], "r");
+    if (du.dim() < 1) raise(PyExc_ValueError, "du must have at least one dimension");
+    const at::ScalarType io = du.scalar_type(), f32 = at::kFloat, res = r.scalar_type();
+    const int32_t code = io_code(du);
+    const at::Device dev = gpu_of(du, "du");
+    const c10::DeviceGuard guard(dev);
+    if (res != io && res != f32)
+        raise(PyExc_TypeError, "r must have dtype %s or Float, got %s", c10::toString(io), c10::toString(res));
+    int64_t tokens;
+    const int64_t D = du.size(-1);
+    const int32_t Dm = size32(D, "d_model");
+    const Sizes lead = leading(du, &tokens);
+    void *pdu = ptr(a[0], "du", io, du.sizes()), *pr = ptr_on(dev, a[1], "r", res, du.sizes());
+    void *pg = ptr_on(dev, a[2], "gamma", f32, {D}), *pm = ptr_on(dev, a[3], "mean", f32, lead);
+    void *ps = ptr_on(dev, a[4], "rstd", f32, lead), *pd = ptr_on(dev, a[5], "d_sum", res, du.sizes());
+    if (res == io && a[7] != Py_None) raise(PyExc_ValueError, "dx_io is written only where r has another type than du");
+    const bool weights = truth(a[12]);
+    const Workspace ws = workspace_on(a[10], a[10] == Py_None ? swimba_layer_norm_bwd_workspace_bytes(tokens, Dm) : 0, dev);
+    Out dx, dxio, dg, db;
+    take_on(dx, a[6], true, "dx", res, du.sizes(), dev);
+    take_on(dxio, a[7], res != io && truth(a[11]), "dx_io", io, du.sizes(), dev);
+    take_on(dg, a[8], weights, "dgamma", f32, {D}, dev);
+    take_on(db, a[9], weights, "dbeta", f32, {D}, dev);
+    void *const hs = stream();
+    check(unlocked([&] {
+              return swimba_layer_norm_bwd(tokens, Dm, code, res == f32 ? SWIMBA_F32 : SWIMBA_BF16, pdu, pr, (float *)pg,
+                                           (float *)pm, (float *)ps, pd, dx.data, dxio.data, (float *)dg.data, (float *)db.data,
+                                           ws.data, ws.bytes, hs);
+          }), "swimba_layer_norm_bwd");
+    return named(g_norm_grad, {&dx, &dxio, &dg, &db});
+}
+
+// Device pointer of a mask, one byte to a token: bool or uint8.
+void *mask_on(at::Device dev, PyObject *o, c10::IntArrayRef shape)
+{
+    const bool is_bool = o != Py_None && tensor(o, "mask").scalar_type() == at::kBool;
+    return ptr_on(dev, o, "mask", is_bool ? at::kBool : at::kByte, shape);
+}
+
+// router_logits top_k mask per_sequence loss counts prob_mean topk_idx topk_w workspace want_topk
+PyObject *router_balance(PyObject *const *a)
+{
+    const at::Tensor &g = tensor(a[0], "router_logits");
+    const bool per_sequence = truth(a[3]);
+    if (g.dim() < (per_sequence ? 3 : 1))
+        raise(PyExc_ValueError, "router_logits must have at least %d dimensions, got %d", per_sequence ? 3 : 1, (int)g.dim());
+    const at::ScalarType io = g.scalar_type(), f32 = at::kFloat;
+    const int32_t code = io_code(g), k = integer32(a[1], "top_k");
+    const at::Device dev = gpu_of(g, "router_logits");
+    const c10::DeviceGuard guard(dev);
+    int64_t tokens;
+    Sizes lead = leading(g, &tokens);
+    const int64_t E = g.size(-1), groups = per_sequence ? g.size(0) : 1;
+    const int32_t En = size32(E, "nexperts");
+    if (per_sequence) tokens = groups ? tokens / groups : 0;
+    void *pg = ptr(a[0], "router_logits", io, g.sizes()), *pm = mask_on(dev, a[2], lead);
+    const size_t want = a[9] == Py_None ? swimba_router_balance_workspace_bytes(groups, tokens, En) : 0;
+    const bool topk = truth(a[10]);
+    if (k < 1 || k > E || k > SWIMBA_MAX_TOPK)      // before outputs of that size
+        check(swimba_router_balance(groups, tokens, En, k, code, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr,
+                                    nullptr, 0, nullptr), "swimba_router_balance");
+    const Workspace ws = workspace_on(a[9], want, dev);
+    Out loss, counts, prob, idx, w;
+    take_on(loss, a[4], true, "loss", f32, {groups}, dev);
+    take_on(counts, a[5], true, "counts", at::kInt, {groups, E}, dev);
+    take_on(prob, a[6], true, "prob_mean", f32, {groups, E}, dev);
+    lead.push_back(k);
+    take_on(idx, a[7], topk, "topk_idx", at::kInt, lead, dev);
+    take_on(w, a[8], topk, "topk_w", f32, lead, dev);
+    void *const hs = stream();
+    check(unlocked([&] {
+              return swimba_router_balance(groups, tokens, En, k, code, pg, (uint8_t *)pm, (int32_t *)idx.data, (float *)w.data,
+                                           (int32_t *)counts.data, (float *)prob.data, (float *)loss.data, ws.data, ws.bytes, hs);
+          }), "swimba_router_balance");
+    return named(g_balance_out, {&loss, &counts, &prob, &idx, &w});
+}
+
+// router_logits topk_idx d_topk_w counts d_loss mask d_logits top_k
+PyObject *router_bwd(PyObject *const *a)
+{
+    const at::Tensor &g = tensor(a[0], "router_logits");
+    if (g.dim() < 1) raise(PyExc_ValueError, "router_logits must have at least one dimension");
+    const at::ScalarType io = g.scalar_type(), f32 = at::kFloat;
+    const int32_t code = io_code(g);
+    const at::Device dev = gpu_of(g, "router_logits");
+    const c10::DeviceGuard guard(dev);
+    int64_t tokens, groups = 1;
+    Sizes lead = leading(g, &tokens);
+    const int64_t E = g.size(-1);
+    if (a[3] != Py_None) {
+        groups = tensor_of_rank(a[3], "counts", 2).size(0);
+        if (groups != 1 && (g.dim() < 3 || groups != g.size(0)))
+            raise(PyExc_ValueError, "counts must have one row, or one for each of router_logits' first dimension, got %d", (int)groups);
+    }
+    void *pg = ptr(a[0], "router_logits", io, g.sizes()), *pm = mask_on(dev, a[5], lead);
+    void *pc = ptr_on(dev, a[3], "counts", at::kInt, {groups, E}), *pl = ptr_on(dev, a[4], "d_loss", f32, {groups});
+    if ((a[3] == Py_None) != (a[4] == Py_None)) raise(PyExc_ValueError, "counts and d_loss come together");
+    if (groups != 1) tokens = groups ? tokens / groups : 0;
+    // how many experts a token has: by the indices, or as told (the counts alone do not say)
+    int64_t k = 1;
+    if (a[1] != Py_None) {
+        k = tensor_of_rank(a[1], "topk_idx", g.dim()).size(-1);
+        if (a[7] != Py_None && integer32(a[7], "top_k") != k) raise(PyExc_ValueError, "top_k is not that of topk_idx");
+    } else if (a[2] != Py_None) {
+        raise(PyExc_ValueError, "d_topk_w needs topk_idx");
+    } else if (a[7] != Py_None) {
+        k = integer32(a[7], "top_k");
+    } else if (a[3] != Py_None) {
+        raise(PyExc_ValueError, "counts need topk_idx or top_k");
+    }
+    lead.push_back(k);
+    void *pi = ptr_on(dev, a[1], "topk_idx", at::kInt, lead), *pw = ptr_on(dev, a[2], "d_topk_w", f32, lead);
+    Out out;
+    take_on(out, a[6], true, "d_logits", io, g.sizes(), dev);
+    void *const hs = stream();
+    const int32_t En = size32(E, "nexperts"), kn = size32(k, "top_k");
+    check(unlocked([&] {
+              return swimba_router_bwd(groups, tokens, En, kn, code, pg, (uint8_t *)pm, (int32_t *)pi, (float *)pw, (int32_t *)pc,
+                                       (float *)pl, out.data, hs);
+          }), "swimba_router_bwd");
+    return out.release();
+}
+
+// u W_g d_logits du_add du dW_g workspace want_du want_dW_g
+PyObject *router_linear_bwd(PyObject *const *a)
+{
+    const at::Tensor &u = tensor(a[0], "u"), &W = tensor_of_rank(a[1], "W_g", 2);
+    if (u.dim() < 1) raise(PyExc_ValueError, "u must have at least one dimension");
+    const at::ScalarType io = u.scalar_type();
+    const int32_t code = io_code(u);
+    const at::Device dev = gpu_of(u, "u");
+    const c10::DeviceGuard guard(dev);
+    int64_t tokens;
+    Sizes lead = leading(u, &tokens);
+    const int64_t D = u.size(-1), E = W.size(0);
+    const int32_t Dm = size32(D, "d_model"), En = size32(E, "nexperts");
+    lead.push_back(E);
+    void *pu = ptr(a[0], "u", io, u.sizes()), *pW = ptr_on(dev, a[1], "W_g", io, {E, D});
+    void *pl = ptr_on(dev, a[2], "d_logits", io, lead), *pa = ptr_on(dev, a[3], "du_add", io, u.sizes());
+    const Workspace ws = workspace_on(a[6], a[6] == Py_None ? swimba_router_linear_bwd_workspace_bytes(tokens, Dm, En) : 0, dev);
+    Out du, dW;
+    take_on(du, a[4], truth(a[7]), "du", io, u.sizes(), dev);
+    take_on(dW, a[5], truth(a[8]), "dW_g", at::kFloat, {E, D}, dev);
+    void *const hs = stream();
+    check(unlocked([&] {
+              return swimba_router_linear_bwd(tokens, Dm, En, code, pu, pW, pl, pa, du.data, (float *)dW.data, ws.data, ws.bytes, hs);
+          }), "swimba_router_linear_bwd");
+    return named(g_linear_grad, {&du, &dW});
+}
+
 template <PyObject *(*F)(PyObject *const *), Py_ssize_t NARGS>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -389,6 +637,20 @@ PyObject *classes(PyObject *, PyObject *const *args, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
+// training_classes(NormOut, NormGrad, BalanceOut, LinearGrad): what those calls return
+PyObject *training_classes(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 4) {
+        PyErr_SetString(PyExc_TypeError, "four classes expected");
+        return nullptr;
+    }
+    g_norm_out = Py_NewRef(args[0]);
+    g_norm_grad = Py_NewRef(args[1]);
+    g_balance_out = Py_NewRef(args[2]);
+    g_linear_grad = Py_NewRef(args[3]);
+    Py_RETURN_NONE;
+}
+
 #define ENTRY(name, f, n) {name, (PyCFunction)(void (*)(void))entry<f, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     {"classes", (PyCFunction)(void (*)(void))classes, METH_FASTCALL, nullptr},
@@ -399,6 +661,12 @@ PyMethodDef methods[] = {
     ENTRY("mixer_fwd_xe_proj", mixer_fwd_xe_proj, 16),
     ENTRY("step", step<false>, 14),
     ENTRY("step_multi", step<true>, 14),
+    {"training_classes", (PyCFunction)(void (*)(void))training_classes, METH_FASTCALL, nullptr},
+    ENTRY("layer_norm", layer_norm, 11),
+    ENTRY("layer_norm_bwd", layer_norm_bwd, 13),
+    ENTRY("router_balance", router_balance, 11),
+    ENTRY("router_bwd", router_bwd, 8),
+    ENTRY("router_linear_bwd", router_linear_bwd, 9),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,383 @@
+"""Routing with a balance loss, the gradient of the logits and the router's backward pass against their formulas in 64 bits,
+and all calls that train the routing in a row."""
+import pytest
+import torch
+
+from paper_2603_06938_amd import binding as sw
+from train_ref import IO, U, balance, d, half, linear_bwd, norm, picks, routing_bwd, softmax, within
+
+pytestmark = pytest.mark.gpu
+
+# experts: both sides of every power of two that the lanes of a token are made for, odd numbers, the most
+EXPERTS = [(1, 1), (2, 1), (3, 3), (5, 2), (7, 4), (8, 2), (9, 9), (15, 4), (16, 2), (16, 16), (17, 3), (31, 8), (32, 4), (33, 2),
+           (60, 6), (64, 8), (65, 16), (100, 4), (127, 2), (128, 8), (129, 1), (200, 16), (255, 5), (256, 8), (256, 16)]
+
+
+def logits_of(shape, io, seed, ties=False):
+    gen = torch.Generator().manual_seed(seed)
+    z = torch.randint(-2, 3, shape, generator=gen).float() if ties else torch.randn(shape, generator=gen)
+    return (z + (0 if ties else 0.5 * torch.randn(shape[-1], generator=gen))).to(IO[io]).to("cuda:0")
+
+
+def lengths(B, L, seed):
+    n = torch.randint(0, L + 1, (B, 1), generator=torch.Generator().manual_seed(seed))
+    return (torch.arange(L)[None] < n).to("cuda:0")
+
+
+def check_balance(z, k, mask, per_sequence, out):
+    idx = picks(z, k)
+    none = softmax(z)[1]
+    assert torch.equal(out.topk_idx.cpu().long()[~none], idx[~none]), "topk_idx"
+    loss, counts, prob, _, rel = balance(z, k, mask, per_sequence)
+    p, _, relp = softmax(z)
+    within(out.topk_w[~none.to(z.device)], torch.gather(p, -1, idx)[~none], (relp * torch.gather(p, -1, idx))[~none], "topk_w")
+    assert out.counts.dtype == torch.int32 and torch.equal(out.counts.cpu().double(), counts), "counts"
+    within(out.prob_mean, prob, rel * prob, "prob_mean")
+    within(out.loss, loss, (rel + 16 * U) * loss, "loss")
+
+
+@pytest.mark.parametrize("E,k", EXPERTS)
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("ties", [False, True])
+def test_balance(E, k, io, ties):
+    B, L = 3, 131
+    z = logits_of((B, L, E), io, E + k, ties)
+    for mask, per_sequence in ((None, False), (lengths(B, L, E), True), (lengths(B, L, E + 1), False)):
+        out = sw.swimba_router_balance(z, k, mask, per_sequence=per_sequence)
+        assert out.loss.shape == ((B,) if per_sequence else (1,))
+        check_balance(z, k, mask, per_sequence, out)
+    idx, w = sw.swimba_router_topk(z, k)
+    assert torch.equal(idx, out.topk_idx)
+    p, _, relp = softmax(z)
+    assert ((w - out.topk_w).abs().double().cpu() <= 2 * relp * torch.gather(p, -1, picks(z, k))).all()
+
+
+@pytest.mark.parametrize("B,L", [(1, 1), (1, 2), (7, 1), (1, 63), (1, 64), (1, 65), (1, 255), (1, 257), (2, 1000), (300, 3), (5000, 2), (1, 70001), (3, 20011)])
+@pytest.mark.parametrize("E,k", [(8, 2), (16, 2), (64, 6), (100, 3)])
+def test_balance_numbers_of_tokens(B, L, E, k):
+    z = logits_of((B, L, E), "bf16", B * L)
+    for per_sequence in (False, True):
+        out = sw.swimba_router_balance(z, k, None, per_sequence=per_sequence)
+        check_balance(z, k, None, per_sequence, out)
+        again = sw.swimba_router_balance(z, k, None, per_sequence=per_sequence)
+        assert all(torch.equal(a, b) for a, b in zip(out, again)), "two calls differ"
+
+
+def hard_rows(z):
+    """-inf in places, rows of nothing else, rows of the type's lowest value, signed zeros"""
+    E = z.shape[-1]
+    z[:, 0::7, E // 2:] = -torch.inf
+    z[:, 4::13] = torch.finfo(z.dtype).min
+    z[:, 5::13, ::2] = torch.finfo(z.dtype).min
+    z[:, 6::17] = 0.0
+    z[:, 6::17, ::2] = -0.0
+    z[:, 3::11] = -torch.inf
+    return z
+
+
+@pytest.mark.parametrize("E,k", [(2, 1), (8, 2), (16, 4), (24, 3), (64, 8), (256, 8)])
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_masked_logits(E, k, io):
+    B, L = 2, 150
+    z = hard_rows(logits_of((B, L, E), io, E))
+    for per_sequence in (False, True):
+        out = sw.swimba_router_balance(z, k, None, per_sequence=per_sequence)
+        check_balance(z, k, None, per_sequence, out)
+        assert out.topk_idx.min() >= 0 and out.topk_idx.max() < E
+        assert (torch.sort(out.topk_idx, dim=-1).values.diff(dim=-1) > 0).all()
+    c, dl = out.counts, torch.tensor([0.3, -0.1], device="cuda:0")
+    dw = torch.randn(B, L, k, device="cuda:0")
+    idx = picks(z, k).int().to("cuda:0")
+    got = sw.swimba_router_bwd(z, idx, dw, c, dl)
+    ref, bound = routing_bwd(z, idx, dw, c, dl)
+    within(got, ref, bound + half(z.dtype) * (ref.abs() + bound), "d_logits")
+    assert (got[:, 3::11] == 0).all()
+
+
+@pytest.mark.parametrize("E,k", [(8, 2), (64, 4), (100, 2)])
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_padding_holds_anything(E, k, io):
+    """What masked tokens hold reaches nothing but their own topk_idx and topk_w, forward and back."""
+    B, L = 4, 200
+    z = logits_of((B, L, E), io, 3)
+    mask = lengths(B, L, 9)
+    mask[2] = False                                             # a sequence without a token
+    dirty = z.clone()
+    dirty[~mask] = float("nan")
+    dirty[1, -1], dirty[2, 5], dirty[2, 6] = float("inf"), float("-inf"), 3e38
+    mask[1, -1] = False
+    z[1, -1], z[2] = 0, 1
+    for m in (mask, mask.to(torch.uint8)):
+        a = sw.swimba_router_balance(z, k, m, per_sequence=True)
+        b = sw.swimba_router_balance(dirty, k, m, per_sequence=True)
+        assert all(torch.equal(p, q) for p, q in zip(a[:3], b[:3])) and a.loss[2] == 0 and (a.counts[2] == 0).all()
+        assert torch.equal(a.topk_idx[mask], b.topk_idx[mask]) and torch.equal(a.topk_w[mask], b.topk_w[mask])
+        assert b.topk_idx.min() >= 0 and b.topk_idx.max() < E
+        assert (torch.sort(b.topk_idx, dim=-1).values.diff(dim=-1) > 0).all()
+    dl = torch.ones(B, device="cuda:0")
+    dw = torch.randn(B, L, k, device="cuda:0") * mask[..., None]
+    for args in ((None, None), (a.topk_idx, dw)):
+        p = sw.swimba_router_bwd(z, *args, a.counts, dl, mask, top_k=k)
+        q = sw.swimba_router_bwd(dirty, *args, a.counts, dl, mask, top_k=k)
+        assert torch.equal(p, q) and (q[~mask] == 0).all()
+
+
+def test_a_logit_that_is_no_number_stays_in_its_group():
+    z = logits_of((3, 100, 16), "f32", 1)
+    want = sw.swimba_router_balance(z, 2, per_sequence=True)
+    for v in (float("nan"), float("inf")):
+        y = z.clone()
+        y[1, 50, 3] = v
+        got = sw.swimba_router_balance(y, 2, per_sequence=True)
+        assert got.loss[1].isnan() and torch.equal(got.loss[[0, 2]], want.loss[[0, 2]])
+        assert torch.equal(got.prob_mean[[0, 2]], want.prob_mean[[0, 2]]) and torch.equal(got.counts[[0, 2]], want.counts[[0, 2]])
+        back = sw.swimba_router_bwd(y, None, None, want.counts, torch.ones(3, device="cuda:0"), top_k=2)
+        assert back[1, 50].isnan().any() and back.isnan().any(-1).sum() == 1
+
+
+@pytest.mark.parametrize("E,k", EXPERTS)
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_gradient_of_the_logits(E, k, io):
+    B, L = 3, 131
+    z = logits_of((B, L, E), io, E)
+    mask = lengths(B, L, E)
+    dw = torch.randn(B, L, k, device="cuda:0", generator=torch.Generator("cuda:0").manual_seed(E))
+    for m, per_sequence in ((None, False), (mask, True)):
+        out = sw.swimba_router_balance(z, k, m, per_sequence=per_sequence)
+        dl = torch.linspace(0.5, 2.0, out.loss.numel(), device="cuda:0") * 100
+        for args in ((out.topk_idx, dw, out.counts, dl), (out.topk_idx, dw, None, None), (out.topk_idx, None, out.counts, dl)):
+            got = sw.swimba_router_bwd(z, *args, m)
+            ref, bound = routing_bwd(z, *args, m)
+            within(got, ref, bound + half(z.dtype) * (ref.abs() + bound), "d_logits")
+
+
+@pytest.mark.parametrize("B,L", [(1, 1), (300, 3), (1, 70001), (3, 20011), (0, 5), (5, 0)])
+def test_gradient_numbers_of_tokens(B, L):
+    for E, k in ((8, 2), (100, 3)):
+        z = logits_of((B, L, E), "bf16", B + L)
+        if not z.numel():
+            out = sw.swimba_router_balance(z, k, per_sequence=True)
+            assert out.loss.shape == (B,) and (out.loss == 0).all() and (out.counts == 0).all() and (out.prob_mean == 0).all()
+            assert sw.swimba_router_bwd(z, out.topk_idx, out.topk_w, out.counts, out.loss).shape == z.shape
+            continue
+        big = torch.full((z.numel() + 64,), 7.0, dtype=z.dtype, device="cuda:0")
+        out = sw.swimba_router_balance(z, k, per_sequence=True)
+        dw = torch.randn(B, L, k, device="cuda:0")
+        args = (out.topk_idx, dw, out.counts, torch.ones(B, device="cuda:0"))
+        got = sw.swimba_router_bwd(z, *args, d_logits=big[:z.numel()].view(z.shape))
+        ref, bound = routing_bwd(z, *args)
+        within(got, ref, bound + half(z.dtype) * (ref.abs() + bound), "d_logits")
+        assert (big[z.numel():] == 7).all()
+
+
+def test_rows_that_start_at_any_element():
+    """Logits whose first element is 2 or 4 bytes into a line, and outputs likewise."""
+    for io in ("f32", "bf16"):
+        for E in (8, 16, 64):
+            z = logits_of((1, 77, E), io, 5)
+            buf = torch.zeros(z.numel() + 1, dtype=z.dtype, device="cuda:0")
+            off = buf[1:].view(z.shape)
+            off.copy_(z)
+            a, b = sw.swimba_router_balance(z, 2), sw.swimba_router_balance(off, 2)
+            assert torch.equal(a.topk_idx, b.topk_idx) and torch.equal(a.counts, b.counts)
+            check_balance(z, 2, None, False, b)
+            out = torch.zeros(z.numel() + 1, dtype=z.dtype, device="cuda:0")[1:].view(z.shape)
+            one = torch.ones(1, device="cuda:0")
+            p, q = sw.swimba_router_bwd(z, a.topk_idx, a.topk_w, a.counts, one), sw.swimba_router_bwd(off, a.topk_idx, a.topk_w, a.counts, one, d_logits=out)
+            assert torch.equal(p, q)
+
+
+def test_indices_that_repeat_or_name_no_expert():
+    """The same index twice adds both gradients; one outside the experts is passed over."""
+    z = logits_of((1, 50, 24), "f32", 2)
+    idx = torch.randint(0, 24, (1, 50, 3), device="cuda:0", dtype=torch.int32)
+    idx[..., 2] = idx[..., 0]
+    dw = torch.randn(1, 50, 3, device="cuda:0")
+    ref, bound = routing_bwd(z, idx, dw, None, None)
+    within(sw.swimba_router_bwd(z, idx, dw), ref, bound + half(z.dtype) * (ref.abs() + bound), "d_logits")
+    bad, dw2 = idx.clone(), dw.clone()
+    bad[:, ::2, 1] = torch.tensor([-1, 24, 1 << 30, -(1 << 31), 64], device="cuda:0", dtype=torch.int32).repeat(5)
+    dw2[:, ::2, 1] = 0
+    got, want = sw.swimba_router_bwd(z, bad, dw), sw.swimba_router_bwd(z, idx, dw2)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("E,k", [(6, 2), (40, 3)])
+def test_gradient_against_differences(E, k):
+    B, L, h = 2, 30, 1e-4
+    z = logits_of((B, L, E), "f32", E)
+    mask = lengths(B, L, 4)
+    mask[:, 0] = True
+    out = sw.swimba_router_balance(z, k, mask, per_sequence=True)
+    gen = torch.Generator().manual_seed(2)
+    v, c = torch.randn(B, L, E, generator=gen, dtype=torch.float64), torch.randn(B, L, k, generator=gen, dtype=torch.float64)
+    dl = torch.tensor([3.0, -2.0], dtype=torch.float64)
+    on = mask.cpu().double()[..., None]
+    n = on.sum(1)
+
+    def f(a):
+        p = torch.softmax(z.double().cpu() + a * v, -1)
+        share = out.counts.double().cpu() / (k * n)
+        return (dl * E * (share * (p * on).sum(1) / n).sum(1)).sum() + (c * torch.gather(p, 2, out.topk_idx.cpu().long())).sum()
+    slope = (8 * (f(h) - f(-h)) - (f(2 * h) - f(-2 * h))) / (12 * h)
+    got = d(sw.swimba_router_bwd(z, out.topk_idx, c.float().to("cuda:0"), out.counts, dl.float().to("cuda:0"), mask))
+    assert abs((got * v).sum() - slope) <= (got * v).abs().sum() * 1000 * U
+
+
+def test_how_many_experts_a_token_has_is_asked_for():
+    z = logits_of((2, 20, 8), "f32", 2)
+    out = sw.swimba_router_balance(z, 3)
+    one = torch.ones(1, device="cuda:0")
+    a = sw.swimba_router_bwd(z, out.topk_idx, None, out.counts, one)
+    assert torch.equal(a, sw.swimba_router_bwd(z, None, None, out.counts, one, top_k=3))
+    for args, kw in (((None, None, out.counts, one), {}), ((out.topk_idx, None, out.counts, one), dict(top_k=2)),
+                     ((None, out.topk_w), dict(top_k=3)), ((out.topk_idx, None, out.counts), {}), ((out.topk_idx, None, None, one), {})):
+        with pytest.raises(ValueError):
+            sw.swimba_router_bwd(z, *args, **kw)
+    for k in (0, 9):
+        with pytest.raises(sw.SwimbaError):
+            sw.swimba_router_bwd(z, None, None, out.counts, one, top_k=k)
+        with pytest.raises(sw.SwimbaError):
+            sw.swimba_router_balance(z, k)
+    with pytest.raises(ValueError):
+        sw.swimba_router_bwd(z, out.topk_idx, None, out.counts.repeat(3, 1), one.repeat(3))
+
+
+# ---- backward pass of the linear map -----------------------------------------------------------------
+LINEAR = [(1, 1, 1), (1, 8, 1), (3, 7, 2), (5, 33, 5), (17, 64, 8), (31, 100, 9), (32, 128, 16), (33, 129, 17), (64, 256, 31), (65, 768, 8),
+          (127, 500, 32), (129, 1024, 33), (250, 777, 64), (257, 640, 65), (300, 384, 100), (100, 264, 129), (70, 130, 200), (200, 512, 256),
+          (1000, 72, 8), (2051, 40, 24), (4097, 16, 3), (13, 4100, 12), (9, 16384, 8), (2, 40000, 6)]
+
+
+def linear_case(T, D, E, io, seed, whole=False):
+    gen = torch.Generator().manual_seed(seed)
+    t = lambda *s: (torch.randint(-3, 4, s, generator=gen).float() if whole else torch.randn(*s, generator=gen)).to(IO[io]).to("cuda:0")
+    return t(T, D), t(E, D), t(T, E), t(T, D)
+
+
+@pytest.mark.parametrize("T,D,E", LINEAR)
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_linear_backward(T, D, E, io):
+    u, W, g, add = linear_case(T, D, E, io, T + D)
+    for a in (None, add):
+        big = torch.full((T * D + 64,), 7.0, dtype=u.dtype, device="cuda:0")
+        out = sw.swimba_router_linear_bwd(u, W, g, a, du=big[:T * D].view(T, D))
+        (du, dW), (bu, bw) = linear_bwd(u, W, g, a)
+        within(out.du, du, bu + half(u.dtype) * (du.abs() + bu), "du")
+        assert out.dW_g.dtype == torch.float32
+        within(out.dW_g, dW, bw, "dW_g")
+        assert (big[T * D:] == 7).all()
+    again = sw.swimba_router_linear_bwd(u, W, g, add)
+    assert torch.equal(again.du, out.du) and torch.equal(again.dW_g, out.dW_g), "two calls differ"
+    stream = add.clone()
+    assert torch.equal(sw.swimba_router_linear_bwd(u, W, g, stream, du=stream).du, out.du)
+
+
+@pytest.mark.parametrize("T,D,E", [(3000, 200, 8), (5000, 136, 40), (20000, 64, 16), (1500, 520, 70)])
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_linear_backward_in_whole_numbers(T, D, E, io):
+    """Small whole numbers: every sum is exact in fp32, so a token, a column or an expert that is left out or taken twice shows."""
+    u, W, g, _ = linear_case(T, D, E, io, T, whole=True)
+    (du, dW), _ = linear_bwd(u, W, g)
+    assert dW.abs().max() < 2 ** 24
+    out = sw.swimba_router_linear_bwd(u, W, g)
+    assert torch.equal(out.dW_g.double().cpu(), dW)
+    assert torch.equal(out.du.cpu(), du.to(u.dtype))
+
+
+def test_linear_backward_parts():
+    u, W, g, add = linear_case(300, 200, 12, "bf16", 1)
+    both = sw.swimba_router_linear_bwd(u, W, g)
+    a = sw.swimba_router_linear_bwd(u, W, g, want_dW_g=False)
+    b = sw.swimba_router_linear_bwd(u, W, g, want_du=False)
+    assert a.dW_g is None and b.du is None and torch.equal(a.du, both.du) and torch.equal(b.dW_g, both.dW_g)
+    none = sw.swimba_router_linear_bwd(u[:0], W, g[:0], dW_g=torch.ones_like(both.dW_g))
+    assert none.du.shape == (0, 200) and (none.dW_g == 0).all()
+
+
+def test_linear_backward_keeps_rows_apart():
+    """Values that are no numbers reach their own row of du and, in a feature, their own column of dW_g."""
+    u, W, g, _ = linear_case(400, 300, 10, "bf16", 3)
+    want = sw.swimba_router_linear_bwd(u, W, g)
+    bad = u.clone()
+    bad[123, 45] = float("nan")
+    got = sw.swimba_router_linear_bwd(bad, W, g)
+    assert torch.equal(got.du, want.du) and got.dW_g[:, 45].isnan().all()
+    got.dW_g[:, 45] = want.dW_g[:, 45]
+    assert torch.equal(got.dW_g, want.dW_g)
+    bad = g.clone()
+    bad[77, 3] = float("inf")
+    got = sw.swimba_router_linear_bwd(u, W, bad)
+    keep = torch.arange(400, device="cuda:0") != 77
+    assert torch.equal(got.du[keep], want.du[keep]) and not got.du[77].isfinite().any()
+    rows = torch.arange(10, device="cuda:0") != 3
+    assert torch.equal(got.dW_g[rows], want.dW_g[rows])
+
+
+# ---- all of them together ----------------------------------------------------------------------------
+class Step:
+    """The routing of one training step: norm, router, loss, and back to the norm's inputs and every weight."""
+
+    def __init__(self, B, L, D, E, k, io, seed):
+        gen = torch.Generator().manual_seed(seed)
+        t = lambda *s: torch.randn(*s, generator=gen).to("cuda:0")
+        self.k = k
+        self.x, self.residual = t(B, L, D).to(IO[io]), t(B, L, D)
+        self.gamma, self.beta, self.W = 1 + 0.1 * t(D), 0.1 * t(D), (t(E, D) * D ** -0.5).to(IO[io])
+        self.mask = lengths(B, L, seed)
+        self.mask[:, 0] = True
+        self.d_w, self.d_u, self.d_loss = t(B, L, k), t(B, L, D).to(IO[io]), torch.full((B,), 0.7, device="cuda:0")
+
+    def run(self):
+        n = sw.swimba_layer_norm(self.x, self.gamma, self.beta, 1e-5, self.residual, want_stats=True)
+        z = sw.swimba_router_linear(n.u, self.W)
+        b = sw.swimba_router_balance(z, self.k, self.mask, per_sequence=True)
+        dz = sw.swimba_router_bwd(z, b.topk_idx, self.d_w, b.counts, self.d_loss, self.mask)
+        g = sw.swimba_router_linear_bwd(n.u, self.W, dz, self.d_u)
+        m = sw.swimba_layer_norm_bwd(g.du, n.sum, self.gamma, n.mean, n.rstd)
+        return b.loss, b.topk_idx, m.dx, m.dgamma, m.dbeta, g.dW_g
+
+
+def test_a_training_step_against_autograd_in_64_bits():
+    s = Step(3, 70, 96, 12, 3, "f32", 5)
+    loss, idx, dx, dgamma, dbeta, dW = s.run()
+    x, gamma, beta, W = (t.double().cpu().requires_grad_() for t in (s.x.double() + s.residual.double(), s.gamma, s.beta, s.W))
+    m = x.mean(-1, keepdim=True)
+    u = (x - m) / ((x - m).square().mean(-1, keepdim=True) + 1e-5).sqrt() * gamma + beta
+    z = u @ W.t()
+    p = torch.softmax(z, -1)
+    on = s.mask.cpu().double()
+    hit = torch.zeros_like(p).scatter(-1, idx.cpu().long(), 1.0) * on[..., None]
+    n = on.sum(1)
+    l = 12 * (hit.sum(1) / (3 * n)[:, None] * (p * on[..., None]).sum(1) / n[:, None]).sum(1)
+    total = (l * 0.7).sum() + (torch.gather(p, -1, idx.cpu().long()) * s.d_w.double().cpu()).sum() + (u * s.d_u.double().cpu()).sum()
+    total.backward()
+    assert torch.equal(idx.cpu().long(), picks(z, 3))
+    # fp32 through four calls, each some hundred half steps of its largest terms
+    for what, got, want in (("loss", loss, l.detach()), ("dx", dx, x.grad), ("dgamma", dgamma, gamma.grad), ("dbeta", dbeta, beta.grad), ("dW_g", dW, W.grad)):
+        assert (d(got) - want).norm() <= 500 * U * want.norm(), what
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_a_training_step_replays_from_graphs(io):
+    """Two graphs of the step, replayed in turn with eager work between them, give the eager results."""
+    s = Step(2, 150, 768, 8, 2, io, 6)
+    want = s.run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs, outs = [], []
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                outs.append(s.run())
+            graphs.append(g)
+    torch.cuda.current_stream().wait_stream(side)
+    for rep in range(6):
+        for t in outs[rep & 1]:
+            t.zero_()
+        assert all(torch.equal(a, b) for a, b in zip(s.run(), want)), rep      # the same calls, eager
+        graphs[rep & 1].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs[rep & 1], want)), rep
