@@ -5,10 +5,12 @@
 // the backward pass) are taken in fp32, and written once.
 #include "rows.hpp"
 
+#include <type_traits>
+
 namespace swimba {
 
-// A row lies in the registers of WPR waves, 8 NV elements to a lane: piece i of lane l are the elements from 8 (l + 64 WPR i) on.
-// sums of n values over the row's waves, in every lane; `round` alternates so that one barrier a round is enough
+// A row lies in the registers of WPR waves, W NV elements to a lane: piece i of lane l are the elements from W (l + 64 WPR i) on.
+// sums of N values over the row's waves, in every lane; `round` alternates, so that one barrier a round is enough
 template <int WPR, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[N][16], int round)
 {
@@ -28,45 +30,52 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[N][16], int
     }
 }
 
-constexpr int norm_threads(int WPR) { return WPR == 16 ? 1024 : 256; }
+constexpr int norm_threads(int WPR) { return WPR < 4 ? 256 : 64 * WPR; }
+constexpr int rows_per_block(int WPR) { return norm_threads(WPR) / 64 / WPR; }
 
-template <typename T, typename R, int NV, int WPR>
+template <typename T, typename R, int W, int NV, int WPR, bool TAIL>
 __global__ void __launch_bounds__(norm_threads(WPR))
 norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
                 T *__restrict__ u, R *sum, float *__restrict__ mean, float *__restrict__ rstd, int64_t tokens, int D)
 {
     __shared__ float lds[2][1][16];
-    constexpr int RPB = norm_threads(WPR) / 64 / WPR;          // rows a block has at a time
-    const int lane = threadIdx.x % (64 * WPR);
+    constexpr int RPB = rows_per_block(WPR);                   // rows a block has at a time
+    const int lane = threadIdx.x % (64 * WPR), slot = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / WPR;
     const float width = (float)D;
     int round = 0;
-    for (int64_t t = (int64_t)blockIdx.x * RPB + threadIdx.x / (64 * WPR); t < tokens; t += (int64_t)gridDim.x * RPB) {
-        float r[NV][8];
+    for (int64_t t = (int64_t)blockIdx.x * RPB + slot; t < tokens; t += (int64_t)gridDim.x * RPB) {
+        const T *const xr = x + t * D;
+        const R *const rr = residual + t * D;
+        R *const sr = sum + t * D;
+        T *const ur = u + t * D;
+        Piece<T, W> px[NV];
+        Piece<R, W> pr[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int d = 8 * (lane + 64 * WPR * i), n = D - d;
-            load8(r[i], x + t * D + d, n, 0.f);
-            if (residual) {
-                float a[8];
-                load8(a, residual + t * D + d, n, 0.f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) r[i][j] = to_float(from_float<R>(r[i][j] + a[j]));
-                if (sum) store8(sum + t * D + d, r[i], n);
-            }
+            const uint32_t d = W * (lane + 64 * WPR * i);
+            px[i].template load<TAIL>(xr + d, D - (int)d);
+            if (residual) pr[i].template load<TAIL>(rr + d, D - (int)d);
         }
-        float s[1] = {0.f};
+        float r[NV][W], s[1] = {0.f};
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t d = W * (lane + 64 * WPR * i);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[0] += r[i][j];
+            for (int j = 0; j < W; ++j) {
+                r[i][j] = px[i].get(j);
+                if (residual) r[i][j] = to_float(from_float<R>(r[i][j] + pr[i].get(j)));
+                s[0] += r[i][j];
+            }
+            if (sum) store_piece<TAIL>(sr + d, r[i], D - (int)d);
+        }
         row_sums<WPR>(s, lds, round++);
-        const float m = s[0] / width;       // divided, not multiplied: a constant row is centred to zero
+        const float m = s[0] / width;                          // divided, not multiplied: a constant row is centred to zero
         s[0] = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int n = D - 8 * (lane + 64 * WPR * i);
+            const int n = D - W * (lane + 64 * WPR * i);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < W; ++j) {
                 r[i][j] -= m;
                 s[0] += j < n ? r[i][j] * r[i][j] : 0.f;
             }
@@ -79,108 +88,192 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int d = 8 * (lane + 64 * WPR * i), n = D - d;
-            float g[8], b[8];
-            if (gamma) load8(g, gamma + d, n, 0.f);
-            if (beta) load8(b, beta + d, n, 0.f);
+            const uint32_t d = W * (lane + 64 * WPR * i);
+            Piece<float, W> g, b;
+            if (gamma) g.template load<TAIL>(gamma + d, D - (int)d);
+            if (beta) b.template load<TAIL>(beta + d, D - (int)d);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) r[i][j] = r[i][j] * is * (gamma ? g[j] : 1.f) + (beta ? b[j] : 0.f);
-            store8(u + t * D + d, r[i], n);
+            for (int j = 0; j < W; ++j) r[i][j] = r[i][j] * is * (gamma ? g.get(j) : 1.f) + (beta ? b.get(j) : 0.f);
+            store_piece<TAIL>(ur + d, r[i], D - (int)d);
         }
     }
 }
 
-template <typename T, typename R, int NV, int WPR>
+// The rows are walked by as many blocks as keep sums of their own; the next row's pieces are under way while a row is summed.
+template <typename T, typename R, int W, int NV, int WPR, bool TAIL>
 __global__ void __launch_bounds__(norm_threads(WPR))
 norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *__restrict__ gamma,
                 const float *__restrict__ mean, const float *__restrict__ rstd, const R *d_sum, R *dx, T *__restrict__ dx_io,
                 float *__restrict__ part, int64_t tokens, int D)
 {
+    constexpr int RPB = rows_per_block(WPR), SPAN = 64 * WPR * W;
     __shared__ float lds[2][2][16];
-    constexpr int RPB = norm_threads(WPR) / 64 / WPR;
-    const int lane = threadIdx.x % (64 * WPR), slot = threadIdx.x / (64 * WPR);
-    const float inv = 1.0f / (float)D;
-    float dg[NV][8] = {}, db[NV][8] = {};
-    int round = 0;
-    for (int64_t t = (int64_t)blockIdx.x * RPB + slot; t < tokens; t += (int64_t)gridDim.x * RPB) {
-        const float m = mean[t], is = rstd[t];
-        float xh[NV][8], g[NV][8], s[2] = {0.f, 0.f};
+    __shared__ float comb[RPB > 1 ? RPB * 2 * NV * SPAN : 1];
+    const int lane = threadIdx.x % (64 * WPR), slot = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / WPR;
+    const float width = (float)D;
+    const int64_t stride = (int64_t)gridDim.x * RPB;
+    constexpr bool AHEAD = WPR < 16;                           // 1024 threads have no registers for it, nor for the gain
+    float dg[NV][W] = {}, db[NV][W] = {}, w[NV][W];
+    auto gain = [&] {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int d = 8 * (lane + 64 * WPR * i), n = D - d;
-            float w[8];
-            load8(xh[i], r + t * D + d, n, m);
-            load8(g[i], du + t * D + d, n, 0.f);
-            if (gamma) load8(w, gamma + d, n, 0.f);
+            const uint32_t d = W * lane + SPAN * i;
+            Piece<float, W> p;
+            if (gamma) p.template load<TAIL>(gamma + d, D - (int)d);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                xh[i][j] = (xh[i][j] - m) * is;
+            for (int j = 0; j < W; ++j) w[i][j] = gamma ? p.get(j) : 1.f;
+        }
+    };
+    if constexpr (AHEAD) gain();
+    struct Row {
+        Piece<T, W> g[NV];
+        Piece<R, W> x[NV], a[NV];
+        float m, s;
+    };
+    auto fetch = [&](Row &q, int64_t t) __attribute__((always_inline)) {
+        q.m = mean[t];
+        q.s = rstd[t];
+        const R *const row = r + t * D, *const add = d_sum + t * D;
+        const T *const grad = du + t * D;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t d = W * lane + SPAN * i;
+            q.x[i].template load<TAIL>(row + d, D - (int)d);
+            q.g[i].template load<TAIL>(grad + d, D - (int)d);
+            if (AHEAD && d_sum) q.a[i].template load<TAIL>(add + d, D - (int)d);
+        }
+    };
+    Row next;
+    int64_t t = (int64_t)blockIdx.x * RPB + slot;
+    if (AHEAD && t < tokens) fetch(next, t);
+    for (int round = 0; t < tokens; t += stride, ++round) {
+        Row q;
+        if constexpr (AHEAD) {
+            q = next;
+            if (t + stride < tokens) fetch(next, t + stride);
+        } else {
+            fetch(q, t);
+            gain();
+        }
+        float xh[NV][W], g[NV][W], s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int n = D - (W * lane + SPAN * i);
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                xh[i][j] = j < n ? (q.x[i].get(j) - q.m) * q.s : 0.f;
+                g[i][j] = q.g[i].get(j);
                 dg[i][j] += g[i][j] * xh[i][j];
                 db[i][j] += g[i][j];
-                if (gamma) g[i][j] *= w[j];
+                g[i][j] *= w[i][j];
                 s[0] += g[i][j];
                 s[1] += g[i][j] * xh[i][j];
             }
         }
-        row_sums<WPR>(s, lds, round++);
-        const float mg = s[0] * inv, mx = s[1] * inv;
+        row_sums<WPR>(s, lds, round);
+        const float mg = s[0] / width, mx = s[1] / width;
+        R *const out = dx + t * D;
+        T *const out_io = dx_io + t * D;
+        const R *const add = d_sum + t * D;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int d = 8 * (lane + 64 * WPR * i), n = D - d;
-            float a[8];
-            if (d_sum) load8(a, d_sum + t * D + d, n, 0.f);
+            const uint32_t d = W * lane + SPAN * i;
+            if (!AHEAD && d_sum) q.a[i].template load<TAIL>(add + d, D - (int)d);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) g[i][j] = is * (g[i][j] - mg - xh[i][j] * mx) + (d_sum ? a[j] : 0.f);
-            store8(dx + t * D + d, g[i], n);
-            if (dx_io) store8(dx_io + t * D + d, g[i], n);
+            for (int j = 0; j < W; ++j) g[i][j] = q.s * (g[i][j] - mg - xh[i][j] * mx) + (d_sum ? q.a[i].get(j) : 0.f);
+            store_piece<TAIL>(out + d, g[i], D - (int)d);
+            if (dx_io) store_piece<TAIL>(out_io + d, g[i], D - (int)d);
         }
     }
     if (!part) return;
-    // (blocks x RPB, 2, D)
-    float *p = part + ((int64_t)blockIdx.x * RPB + slot) * 2 * D;
+    float *p = part + (int64_t)blockIdx.x * 2 * D;              // (blocks, 2, D)
+    if constexpr (RPB > 1) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int d = 8 * (lane + 64 * WPR * i), n = D - d;
-        store8(p + d, dg[i], n);
-        store8(p + D + d, db[i], n);
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                const int d = W * lane + SPAN * i + j;
+                comb[(slot * 2) * NV * SPAN + d] = dg[i][j];
+                comb[(slot * 2 + 1) * NV * SPAN + d] = db[i][j];
+            }
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * D; c += norm_threads(WPR)) {
+            const int at = c < D ? c : c - D + NV * SPAN;
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < RPB; ++k) s += comb[k * 2 * NV * SPAN + at];
+            p[c] = s;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int d = W * lane + SPAN * i;
+            store_piece<TAIL>(p + d, dg[i], D - d);
+            store_piece<TAIL>(p + D + d, db[i], D - d);
+        }
     }
 }
 
-// out[c] = sum over the rows of part (rows, 2 D), in their order; columns behind D are dbeta's
-__global__ void __launch_bounds__(256)
+// out[c] = sum over the rows of part (rows, 2 D); columns behind D are dbeta's.  32 columns to a block, whose 16 half waves
+// take every 16th row each: a row is a line of memory, and 16 x 8 of them are under way.
+__global__ void __launch_bounds__(512)
 norm_reduce_kernel(const float *__restrict__ part, int rows, int D, float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= 2 * D) return;
+    __shared__ float lds[16][33];
+    const int c = blockIdx.x * 32 + threadIdx.x % 32, slice = threadIdx.x / 32;
     float s = 0.f;
-    for (int i = 0; i < rows; ++i) s += part[(int64_t)i * 2 * D + c];
+    if (c < 2 * D) {
+#pragma unroll 8
+        for (int i = slice; i < rows; i += 16) s += part[(int64_t)i * 2 * D + c];
+    }
+    lds[slice][threadIdx.x % 32] = s;
+    __syncthreads();
+    if (slice || c >= 2 * D) return;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += lds[i][threadIdx.x];
     float *out = c < D ? dgamma : dbeta;
     if (out) out[c < D ? c : c - D] = s;
 }
 
 namespace {
 
-// Rows of one wave up to 1024 features, of four up to 8192, of sixteen up to 16384.
-int waves_per_row(int D) { return D <= 1024 ? 1 : D <= 8192 ? 4 : 16; }
-int rows_per_block(int D) { return D <= 1024 ? 4 : 1; }
+// Waves of a row, so that a lane has 16 elements at most: one up to 1024 features, then four, eight and sixteen.
+int waves_per_row(int D) { return D <= 1024 ? 1 : D <= 4096 ? 4 : D <= 8192 ? 8 : 16; }
+
+// f(number of pieces, waves of a row, whether the last piece may be short) as constants
+template <int W, typename F>
+void with_row(int D, F &&f)
+{
+    using std::integral_constant;
+    const int wpr = waves_per_row(D), nv = (D + 64 * wpr * W - 1) / (64 * wpr * W);
+    auto tail = [&](auto n, auto waves) {
+        if (D % W) f(n, waves, std::true_type());
+        else f(n, waves, std::false_type());
+    };
+    constexpr integral_constant<int, 16 / W> most;
+    constexpr integral_constant<int, 8 / W> some;
+    if (wpr == 16) return tail(most, integral_constant<int, 16>());
+    if (wpr == 8) return tail(most, integral_constant<int, 8>());
+    if (wpr == 4) return nv > some ? tail(most, integral_constant<int, 4>()) : tail(some, integral_constant<int, 4>());
+    constexpr integral_constant<int, 1> one;
+    if (nv > 12 / W) return tail(most, one);
+    if (nv > 8 / W) return tail(integral_constant<int, (12 + W - 1) / W>(), one);
+    return nv > 4 / W ? tail(some, one) : tail(integral_constant<int, (4 + W - 1) / W>(), one);
+}
+
+constexpr int NORM_W = 4;                  // elements of a piece
 
 template <typename T, typename R>
 swimba_status norm_fwd(int64_t tokens, int D, const void *x, const void *residual, const float *gamma, const float *beta,
                        float eps, void *u, void *sum, float *mean, float *rstd, hipStream_t st)
 {
-    const int wpr = waves_per_row(D), rpb = rows_per_block(D);
-    const int64_t need = (tokens + rpb - 1) / rpb;
-    const unsigned grid = (unsigned)(need < (1 << 20) ? need : (1 << 20));
-    auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(norm_threads(wpr)), 0, st, (const T *)x, (const R *)residual, gamma, beta, eps,
-                           (T *)u, (R *)sum, mean, rstd, tokens, D);
-    };
-    if (D <= 512) go(norm_fwd_kernel<T, R, 1, 1>);
-    else if (D <= 1024) go(norm_fwd_kernel<T, R, 2, 1>);
-    else if (D <= 2048) go(norm_fwd_kernel<T, R, 1, 4>);
-    else if (D <= 4096) go(norm_fwd_kernel<T, R, 2, 4>);
-    else if (D <= 8192) go(norm_fwd_kernel<T, R, 4, 4>);
-    else go(norm_fwd_kernel<T, R, 2, 16>);
+    with_row<NORM_W>(D, [&](auto nv, auto wpr, auto tail) {
+        const int64_t need = (tokens + rows_per_block(wpr) - 1) / rows_per_block(wpr);
+        hipLaunchKernelGGL((norm_fwd_kernel<T, R, NORM_W, nv(), wpr(), tail()>), dim3((unsigned)(need < (1 << 20) ? need : (1 << 20))),
+                           dim3(norm_threads(wpr)), 0, st, (const T *)x, (const R *)residual, gamma, beta, eps, (T *)u, (R *)sum, mean,
+                           rstd, tokens, D);
+    });
     SWIMBA_CHECK_LAUNCH();
     return SWIMBA_OK;
 }
@@ -188,7 +281,7 @@ swimba_status norm_fwd(int64_t tokens, int D, const void *x, const void *residua
 // most blocks of the backward pass, which keep sums of their own
 int64_t bwd_blocks(int64_t tokens, int D)
 {
-    const int rpb = rows_per_block(D);
+    const int rpb = rows_per_block(waves_per_row(D));
     const int64_t need = (tokens + rpb - 1) / rpb, most = waves_per_row(D) == 16 ? 256 : 512;
     return need < most ? need : most;
 }
@@ -197,28 +290,18 @@ template <typename T, typename R>
 swimba_status norm_bwd(int64_t tokens, int D, const void *du, const void *r, const float *gamma, const float *mean,
                        const float *rstd, const void *d_sum, void *dx, void *dx_io, float *part, hipStream_t st)
 {
-    const int wpr = waves_per_row(D);
-    const unsigned grid = (unsigned)bwd_blocks(tokens, D);
-    auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(norm_threads(wpr)), 0, st, (const T *)du, (const R *)r, gamma, mean, rstd,
-                           (const R *)d_sum, (R *)dx, (T *)dx_io, part, tokens, D);
-    };
-    if (D <= 512) go(norm_bwd_kernel<T, R, 1, 1>);
-    else if (D <= 1024) go(norm_bwd_kernel<T, R, 2, 1>);
-    else if (D <= 2048) go(norm_bwd_kernel<T, R, 1, 4>);
-    else if (D <= 4096) go(norm_bwd_kernel<T, R, 2, 4>);
-    else if (D <= 8192) go(norm_bwd_kernel<T, R, 4, 4>);
-    else go(norm_bwd_kernel<T, R, 2, 16>);
+    with_row<NORM_W>(D, [&](auto nv, auto wpr, auto tail) {
+        hipLaunchKernelGGL((norm_bwd_kernel<T, R, NORM_W, nv(), wpr(), tail()>), dim3((unsigned)bwd_blocks(tokens, D)),
+                           dim3(norm_threads(wpr)), 0, st, (const T *)du, (const R *)r, gamma, mean, rstd, (const R *)d_sum, (R *)dx,
+                           (T *)dx_io, part, tokens, D);
+    });
     SWIMBA_CHECK_LAUNCH();
     return SWIMBA_OK;
 }
 
 }  // namespace
 
-size_t layer_norm_bwd_bytes(int64_t tokens, int D)
-{
-    return (size_t)bwd_blocks(tokens, D) * rows_per_block(D) * 2 * D * sizeof(float);
-}
+size_t layer_norm_bwd_bytes(int64_t tokens, int D) { return (size_t)bwd_blocks(tokens, D) * 2 * D * sizeof(float); }
 
 swimba_status launch_layer_norm(int64_t tokens, int D, int io_dtype, int res_dtype, const void *x, const void *residual,
                                 const float *gamma, const float *beta, float eps, void *u, void *sum, float *mean, float *rstd,
@@ -240,8 +323,8 @@ swimba_status launch_layer_norm_bwd(int64_t tokens, int D, int io_dtype, int res
         if (s != SWIMBA_OK) return s;
     }
     if (sums) {
-        hipLaunchKernelGGL(norm_reduce_kernel, dim3((unsigned)((2 * D + 255) / 256)), dim3(256), 0, st, part,
-                           (int)(bwd_blocks(tokens, D) * rows_per_block(D)), D, dgamma, dbeta);
+        hipLaunchKernelGGL(norm_reduce_kernel, dim3((unsigned)((2 * D + 31) / 32)), dim3(512), 0, st, part,
+                           (int)bwd_blocks(tokens, D), D, dgamma, dbeta);
         SWIMBA_CHECK_LAUNCH();
     }
     return SWIMBA_OK;

@@ -12,44 +12,67 @@ namespace swimba {
 typedef uint32_t __attribute__((ext_vector_type(4), aligned(2))) any_u32x4_t;
 typedef uint32_t __attribute__((ext_vector_type(2), aligned(2))) any_u32x2_t;
 
-// eight consecutive elements from and to memory, as floats
-__device__ __forceinline__ void load8(float (&f)[8], const bf16 *p)
-{
-    const any_u32x4_t v = *reinterpret_cast<const any_u32x4_t *>(p);
-    unpack8(f, make_uint4(v.x, v.y, v.z, v.w));
-}
-__device__ __forceinline__ void load8(float (&f)[8], const float *p)
-{
-    const any_u32x4_t a = *reinterpret_cast<const any_u32x4_t *>(p), b = *reinterpret_cast<const any_u32x4_t *>(p + 4);
+// W (4 or 8) consecutive elements of a row as they lie in memory: loaded long before they are used, they take few registers.
+template <typename T, int W> struct Piece {
+    static constexpr int WORDS = W * (int)sizeof(T) / 4;
+    uint32_t v[WORDS];
+    // the first n of the elements (n <= 0: none); the others become zero.  TAIL: n may lie between 0 and W
+    template <bool TAIL> __device__ __forceinline__ void load(const T *p, int n)
+    {
+        if (n >= W) {
+            if constexpr (WORDS == 2) {
+                const any_u32x2_t a = *reinterpret_cast<const any_u32x2_t *>(p);
+                v[0] = a.x; v[1] = a.y;
+            } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { f[i] = __uint_as_float(a[i]); f[4 + i] = __uint_as_float(b[i]); }
-}
-__device__ __forceinline__ void store8(bf16 *p, const float (&f)[8])
-{
-    const uint4 v = pack8(f);
-    *reinterpret_cast<any_u32x4_t *>(p) = any_u32x4_t{v.x, v.y, v.z, v.w};
-}
-__device__ __forceinline__ void store8(float *p, const float (&f)[8])
-{
-    any_u32x4_t a, b;
+                for (int i = 0; i < WORDS; i += 4) {
+                    const any_u32x4_t a = *reinterpret_cast<const any_u32x4_t *>(p + i * 4 / sizeof(T));
+                    v[i] = a.x; v[i + 1] = a.y; v[i + 2] = a.z; v[i + 3] = a.w;
+                }
+            }
+            return;
+        }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { a[i] = __float_as_uint(f[i]); b[i] = __float_as_uint(f[4 + i]); }
-    *reinterpret_cast<any_u32x4_t *>(p) = a;
-    *reinterpret_cast<any_u32x4_t *>(p + 4) = b;
-}
-// the first n of them (n <= 0: none), the others as `rest` / left alone
-template <typename T> __device__ __forceinline__ void load8(float (&f)[8], const T *p, int n, float rest)
-{
-    if (n >= 8) return load8(f, p);
+        for (int i = 0; i < WORDS; ++i) v[i] = 0;
+        if constexpr (TAIL) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = i < n ? to_float(p[i]) : rest;
-}
-template <typename T> __device__ __forceinline__ void store8(T *p, const float (&f)[8], int n)
+            for (int i = 0; i < W - 1; ++i)
+                if (i < n) {
+                    if constexpr (sizeof(T) == 2) v[i / 2] |= (uint32_t)p[i].bits << (i % 2 * 16);
+                    else v[i] = __float_as_uint(p[i]);
+                }
+        }
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(v[i]);
+        else return i % 2 ? bf_hi(v[i / 2]) : bf_lo(v[i / 2]);
+    }
+};
+
+// the first n of W floats to a row, rounded to its type
+template <bool TAIL, typename T, int W> __device__ __forceinline__ void store_piece(T *p, const float (&f)[W], int n)
 {
-    if (n >= 8) return store8(p, f);
+    if (n >= W) {
+        uint32_t v[Piece<T, W>::WORDS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < n) p[i] = from_float<T>(f[i]);
+        for (int i = 0; i < Piece<T, W>::WORDS; ++i) {
+            if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(f[i]);
+            else v[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+        }
+        if constexpr (Piece<T, W>::WORDS == 2) *reinterpret_cast<any_u32x2_t *>(p) = any_u32x2_t{v[0], v[1]};
+        else {
+#pragma unroll
+            for (int i = 0; i < Piece<T, W>::WORDS; i += 4)
+                *reinterpret_cast<any_u32x4_t *>(p + i * 4 / sizeof(T)) = any_u32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
+        }
+        return;
+    }
+    if constexpr (TAIL) {
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i)
+            if (i < n) p[i] = from_float<T>(f[i]);
+    }
 }
 
 // sum over the 64 lanes, in every lane
