@@ -214,26 +214,14 @@ norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *
     }
 }
 
-// out[c] = sum over the rows of part (rows, 2 D); columns behind D are dbeta's.  32 columns to a block, whose 16 half waves
-// take every 16th row each: a row is a line of memory, and 16 x 8 of them are under way.
+// the blocks' sums joined; columns behind D are dbeta's
 __global__ void __launch_bounds__(512)
 norm_reduce_kernel(const float *__restrict__ part, int rows, int D, float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
-    __shared__ float lds[16][33];
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, slice = threadIdx.x / 32;
-    float s = 0.f;
-    if (c < 2 * D) {
-#pragma unroll 8
-        for (int i = slice; i < rows; i += 16) s += part[(int64_t)i * 2 * D + c];
-    }
-    lds[slice][threadIdx.x % 32] = s;
-    __syncthreads();
-    if (slice || c >= 2 * D) return;
-    s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s += lds[i][threadIdx.x];
-    float *out = c < D ? dgamma : dbeta;
-    if (out) out[c < D ? c : c - D] = s;
+    sum_rows(part, rows, 2 * D, [&](int64_t c, float s) {
+        float *out = c < D ? dgamma : dbeta;
+        if (out) out[c < D ? c : c - D] = s;
+    });
 }
 
 namespace {

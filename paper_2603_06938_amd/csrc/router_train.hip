@@ -1,9 +1,7 @@
-// Training the router: routing with per-expert counts and a balance loss, the gradient of the logits, and the backward pass of
-// the router's linear map.
+// Training the router: routing with per-expert counts and a balance loss, and the gradient of the logits.
 //   balance   pi = softmax(logits), K = top-k;  counts[e] = #{t : e in K_t}, P[e] = mean_t pi_t[e],  loss = E sum_e f_e P_e with
 //             f_e = counts[e] / (k n), over the n tokens of a group that count
 //   logits    g_t[e] = [e in K_t] dw + d_loss (E / n) f_e,   d_logits = pi (g - <pi, g>)
-//   linear    du = d_logits W_g + du_add,   dW_g = d_logits^T u
 #include "rows.hpp"
 
 namespace swimba {
@@ -187,81 +185,6 @@ swimba_status launch_router_bwd(int64_t groups, int64_t tokens, int E, int K, in
                            d_loss, (float *)d_logits, tokens, per_group, E, K);
     SWIMBA_CHECK_LAUNCH();
     return SWIMBA_OK;
-}
-
-// ---- backward pass of the linear map ------------------------------------------------------------------------------------
-constexpr int64_t RLB_SLICE = 512, RLB_SLICES = 64;            // tokens of a slice of dW_g, most slices
-static int64_t linear_slices(int64_t tokens)
-{
-    const int64_t n = (tokens + RLB_SLICE - 1) / RLB_SLICE;
-    return n < RLB_SLICES ? n : RLB_SLICES;
-}
-
-template <typename T>
-__global__ void __launch_bounds__(256)
-linear_du_kernel(const T *__restrict__ Wg, const T *__restrict__ dl, const T *du_add, T *du, int64_t tokens, int D, int E)
-{
-    const int64_t t = blockIdx.y + (int64_t)blockIdx.z * 65535;
-    const int d = blockIdx.x * 256 + threadIdx.x;
-    if (t >= tokens || d >= D) return;
-    float s = 0.f;
-    for (int e = 0; e < E; ++e) s += to_float(dl[t * E + e]) * to_float(Wg[(int64_t)e * D + d]);
-    if (du_add) s += to_float(du_add[t * D + d]);
-    du[t * D + d] = from_float<T>(s);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(256)
-linear_dw_kernel(const T *__restrict__ u, const T *__restrict__ dl, float *__restrict__ part, int64_t tokens, int D, int E)
-{
-    const int d = blockIdx.x * 256 + threadIdx.x, e = blockIdx.y, slices = gridDim.z;
-    if (d >= D) return;
-    const int64_t n = (tokens + slices - 1) / slices, t0 = blockIdx.z * n, t1 = t0 + n < tokens ? t0 + n : tokens;
-    float s = 0.f;
-    for (int64_t t = t0; t < t1; ++t) s += to_float(dl[t * E + e]) * to_float(u[t * D + d]);
-    part[((int64_t)blockIdx.z * E + e) * D + d] = s;
-}
-
-__global__ void __launch_bounds__(256)
-linear_reduce_kernel(const float *__restrict__ part, int slices, int64_t n, float *__restrict__ dW)
-{
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    float s = 0.f;
-    for (int k = 0; k < slices; ++k) s += part[k * n + i];
-    dW[i] = s;
-}
-
-size_t router_linear_bwd_bytes(int64_t tokens, int D, int E) { return (size_t)linear_slices(tokens) * E * D * sizeof(float); }
-
-template <typename T>
-static swimba_status linear_bwd(int64_t tokens, int D, int E, const void *u, const void *Wg, const void *dl, const void *du_add,
-                                void *du, float *dW, float *part, hipStream_t st)
-{
-    const unsigned cols = (unsigned)((D + 255) / 256);
-    const int slices = (int)linear_slices(tokens);
-    if (du && tokens > 0) {
-        hipLaunchKernelGGL(linear_du_kernel<T>, dim3(cols, (unsigned)(tokens < 65535 ? tokens : 65535), (unsigned)((tokens + 65534) / 65535)),
-                           dim3(256), 0, st, (const T *)Wg, (const T *)dl, (const T *)du_add, (T *)du, tokens, D, E);
-        SWIMBA_CHECK_LAUNCH();
-    }
-    if (dW) {
-        if (slices > 0) {
-            hipLaunchKernelGGL(linear_dw_kernel<T>, dim3(cols, (unsigned)E, (unsigned)slices), dim3(256), 0, st, (const T *)u,
-                               (const T *)dl, part, tokens, D, E);
-            SWIMBA_CHECK_LAUNCH();
-        }
-        const int64_t n = (int64_t)E * D;
-        hipLaunchKernelGGL(linear_reduce_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, part, slices, n, dW);
-        SWIMBA_CHECK_LAUNCH();
-    }
-    return SWIMBA_OK;
-}
-
-swimba_status launch_router_linear_bwd(int64_t tokens, int D, int E, int io_dtype, const void *u, const void *Wg, const void *dl,
-                                       const void *du_add, void *du, float *dW, void *part, hipStream_t st)
-{
-    return (io_dtype == SWIMBA_BF16 ? linear_bwd<bf16> : linear_bwd<float>)(tokens, D, E, u, Wg, dl, du_add, du, dW, (float *)part, st);
 }
 
 }  // namespace swimba

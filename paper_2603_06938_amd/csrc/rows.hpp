@@ -11,6 +11,7 @@ namespace swimba {
 // written in one piece all the same.
 typedef uint32_t __attribute__((ext_vector_type(4), aligned(2))) any_u32x4_t;
 typedef uint32_t __attribute__((ext_vector_type(2), aligned(2))) any_u32x2_t;
+typedef uint32_t __attribute__((aligned(2))) any_u32_t;
 
 // W (4 or 8) consecutive elements of a row as they lie in memory: loaded long before they are used, they take few registers.
 template <typename T, int W> struct Piece {
@@ -73,6 +74,28 @@ template <bool TAIL, typename T, int W> __device__ __forceinline__ void store_pi
         for (int i = 0; i < W - 1; ++i)
             if (i < n) p[i] = from_float<T>(f[i]);
     }
+}
+
+// out[c] = sum over `rows` rows of part (rows, n), c < n, in an order that the sizes alone decide.  32 columns to a block of 512
+// threads, whose 16 half waves take every 16th row each: a piece of a row is a line of memory, and up to 16 x 8 are under way.
+template <typename Store>
+__device__ __forceinline__ void sum_rows(const float *__restrict__ part, int rows, int64_t n, Store store)
+{
+    __shared__ float lds[16][33];
+    const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x % 32;
+    const int slice = threadIdx.x / 32;
+    float s = 0.f;
+    if (c < n) {
+#pragma unroll 8
+        for (int i = slice; i < rows; i += 16) s += part[i * n + c];
+    }
+    lds[slice][threadIdx.x % 32] = s;
+    __syncthreads();
+    if (slice || c >= n) return;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += lds[i][threadIdx.x];
+    store(c, s);
 }
 
 // sum over the 64 lanes, in every lane
