@@ -5,8 +5,6 @@
 // the backward pass) are taken in fp32, and written once.
 #include "rows.hpp"
 
-#include <type_traits>
-
 namespace swimba {
 
 // A row lies in the registers of WPR waves, W NV elements to a lane: piece i of lane l are the elements from W (l + 64 WPR i) on.

@@ -5,6 +5,8 @@
 #include "common.hpp"
 #include "mfma_util.hpp"
 
+#include <type_traits>
+
 namespace swimba {
 
 // 16 and 8 bytes at an address that is a multiple of the element size only (rows of an odd width): global memory is read and
@@ -98,12 +100,44 @@ __device__ __forceinline__ void sum_rows(const float *__restrict__ part, int row
     store(c, s);
 }
 
-// sum over the 64 lanes, in every lane
-__device__ __forceinline__ float wave_sum(float v)
+// The value of the lane at distance D, once the lanes at smaller distances agree (for D = 4 and 8 another lane of those
+// stands in).  Register moves, no LDS pass.
+template <int D>
+__device__ __forceinline__ uint32_t partner(uint32_t v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    static_assert(D == 1 || D == 2 || D == 4 || D == 8, "inside a row of 16 lanes");
+    constexpr int ctrl = D == 1 ? 0xB1 : D == 2 ? 0x4E : D == 4 ? 0x141 : 0x128;   // quad_perm, half mirror, row_ror:8
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, true);
+}
+// op over lanes whose numbers differ in the bits from FROM to below TO, in every one of them
+template <int FROM, int TO, typename Op>
+__device__ __forceinline__ uint32_t over_lanes(uint32_t v, Op op)
+{
+    if constexpr (FROM < TO) {
+        if constexpr (FROM >= 16) {
+            const auto r = FROM == 16 ? __builtin_amdgcn_permlane16_swap(v, v, false, false) : __builtin_amdgcn_permlane32_swap(v, v, false, false);
+            v = op(r[0], r[1]);
+        } else if constexpr (FROM == 4) {
+            v = op(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x101f));          // xor 4
+        } else
+            v = op(v, partner<FROM>(v));
+        return over_lanes<FROM * 2, TO>(v, op);
+    }
     return v;
 }
+// the same over the lanes of an aligned group of G
+template <int G, typename Op>
+__device__ __forceinline__ uint32_t over_group(uint32_t v, Op op)
+{
+    if constexpr (G > 1) v = op(v, partner<1>(v));
+    if constexpr (G > 2) v = op(v, partner<2>(v));
+    if constexpr (G > 4) v = op(v, partner<4>(v));
+    return over_lanes<8, G>(v, op);
+}
+__device__ __forceinline__ uint32_t add_f32(uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }
+template <int G> __device__ __forceinline__ float group_sum(float v) { return __uint_as_float(over_group<G>(__float_as_uint(v), add_f32)); }
+
+// sum over the 64 lanes, in every lane
+__device__ __forceinline__ float wave_sum(float v) { return group_sum<64>(v); }
 
 }  // namespace swimba
