@@ -8,107 +8,119 @@
 
 namespace swimba {
 
-constexpr int RT_MOST = 1024;              // threads of the largest block
-
-// Order of logits as unsigned numbers: -0 as +0, NaN outside the numbers by sign.
+// Order of 16-bit pairs of bf16 bits as unsigned numbers: -0 as +0, NaN outside the numbers by sign.
+__device__ __forceinline__ uint32_t order_of_pair(uint32_t u)
+{
+    typedef int16_t __attribute__((ext_vector_type(2))) s16x2;
+    const uint32_t neg = __builtin_bit_cast(uint32_t, __builtin_bit_cast(s16x2, u) >> (int16_t)15);
+    const uint32_t add = (neg & 0x80018001u) ^ 0x80008000u;            // positive u: u + 2^15; negative: ~u + 1
+    return __builtin_bit_cast(uint32_t, (s16x2)(__builtin_bit_cast(s16x2, u ^ neg) + __builtin_bit_cast(s16x2, add)));
+}
 __device__ __forceinline__ uint32_t order_of(float f)
 {
     const uint32_t u = __float_as_uint(f + 0.0f);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float of_order(uint32_t s) { return __uint_as_float(s & 0x80000000u ? s ^ 0x80000000u : ~s); }
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint32_t umin(uint32_t a, uint32_t b) { return a < b ? a : b; }
 
-// One token in G lanes.  Keys are larger the earlier an expert is picked, and 0 past the last expert; bf16 logits leave room for
-// the expert in the lower half, so that their keys are all different and carry it.
-template <typename T, int G> struct Token {
-    static constexpr bool PACKED = sizeof(T) == 2;
-    static constexpr int ROUNDS = 8 * G < SWIMBA_MAX_TOPK ? 8 * G : SWIMBA_MAX_TOPK, SLOTS = (ROUNDS + G - 1) / G;
-    float f[8];
-    uint32_t key[8];
-    __device__ __forceinline__ void take(const Piece<T, 8> &p, int l, int E)
+// One token in G lanes, 8 NP experts to a lane: piece i of lane l are the experts from 8 (l + G i) on.
+// A key is larger the earlier its expert is picked, and 0 past the last expert.  Its lowest bits are the expert's, counted
+// down, so that all keys differ and name their experts; above them lie all 16 bits of a bf16 logit's order, or the upper 24 of
+// an fp32 one's, which do not decide between logits that agree that far: those are picked by the whole of them (`close`).
+// FULL: the experts fill the lanes.
+template <typename T, int NP, int G, bool FULL> struct Token {
+    static constexpr bool BF = sizeof(T) == 2;
+    static constexpr int SIZE = 8 * NP * G, ROUNDS = SIZE < SWIMBA_MAX_TOPK ? SIZE : SWIMBA_MAX_TOPK, SLOTS = (ROUNDS + G - 1) / G;
+    static constexpr uint32_t LOW = BF ? 0xffffu : 0xffu;
+    const Piece<T, 8> (&p)[NP];
+    const int l, E;
+    uint32_t key[NP][8], best;
+    float top;                                                 // largest logit
+
+    __device__ __forceinline__ int expert(int i, int j) const { return 8 * (l + G * i) + j; }
+    __device__ __forceinline__ bool real(int i, int j) const { return FULL || expert(i, j) < E; }
+    __device__ __forceinline__ Token(const Piece<T, 8> (&pieces)[NP], int lane, int experts) : p(pieces), l(lane), E(experts)
     {
+        uint32_t most = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            f[j] = p.get(j);
-            const uint32_t s = order_of(f[j]);
-            key[j] = 8 * l + j >= E ? 0 : PACKED ? (s & 0xffff0000u) | (uint32_t)(0xffff - 8 * l - j) : s > 1 ? s : 1;
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t low = LOW - expert(i, j);
+                uint32_t k;
+                if constexpr (BF) {
+                    const uint32_t s = order_of_pair(p[i].v[j / 2]);
+                    k = j % 2 ? (s & 0xffff0000u) | low : s << 16 | low;
+                } else {
+                    const uint32_t s = order_of(p[i].get(j));
+                    most = umax(most, real(i, j) ? s : 0);
+                    k = (s & ~LOW) | low;
+                }
+                key[i][j] = real(i, j) ? k : 0;
+            }
+        best = over([&](int i, int j) { return key[i][j]; }, umax);
+        if constexpr (BF) {
+            const uint32_t s = best >> 16;
+            top = __uint_as_float((s & 0x8000u ? s ^ 0x8000u : 0u - s) << 16);
+        } else {
+            most = over_group<G>(most, umax);
+            top = __uint_as_float(most & 0x80000000u ? most ^ 0x80000000u : ~most);
         }
     }
-    static __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
-    static __device__ __forceinline__ uint32_t umin(uint32_t a, uint32_t b) { return a < b ? a : b; }
-    __device__ __forceinline__ uint32_t first() const
+    template <typename F> __device__ __forceinline__ uint32_t over(F f, uint32_t (*op)(uint32_t, uint32_t)) const
     {
-        uint32_t b = key[0];
+        uint32_t v = f(0, 0);
 #pragma unroll
-        for (int j = 1; j < 8; ++j) b = umax(b, key[j]);
-        return over_group<G>(b, umax);
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v = op(v, f(i, j));
+        return over_group<G>(v, op);
     }
     // largest key below `best`: at the smallest distance under it, those at and above it being far away
     __device__ __forceinline__ uint32_t next(uint32_t best) const
     {
-        uint32_t d = best - 1 - key[0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) d = umin(d, best - 1 - key[j]);
-        return best - 1 - over_group<G>(d, umin);
+        return best - 1 - over([&](int i, int j) { return best - 1 - key[i][j]; }, umin);
     }
-    // lowest expert behind `after` with this key; a number past all experts where there is none
-    __device__ __forceinline__ int holder(uint32_t best, int after, int l) const
-    {
-        uint32_t e = 1 << 20;
-#pragma unroll
-        for (int j = 7; j >= 0; --j)
-            if (key[j] == best && 8 * l + j > after) e = 8 * l + j;
-        return (int)over_group<G>(e, umin);
-    }
-    static __device__ __forceinline__ float value(uint32_t k)
-    {
-        return PACKED ? __uint_as_float(__float_as_uint(of_order(k)) & 0xffff0000u) : of_order(k);
-    }
+    static __device__ __forceinline__ int expert_of(uint32_t k) { return (int)(LOW - (k & LOW)); }
 
-    // The K picks: lane l keeps those of rounds l, l + G, ... in (e, k); bit j of the result: the lane's expert j is one of them.
-    __device__ __forceinline__ uint32_t picks(uint32_t best, int K, int l, int (&e)[SLOTS], uint32_t (&k)[SLOTS]) const
+    // The K picks: lane l keeps the experts of rounds l, l + G, ...
+    __device__ __forceinline__ void picks(int K, int (&e)[SLOTS]) const
     {
         uint32_t b = best;
-        bool falls = true;
+        bool close = false;
 #pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) {
-            if (r < K) {
-                if (r) {
-                    const uint32_t n = next(b);
-                    falls = falls && n < b;
-                    b = n;
-                }
-                const int x = PACKED ? (int)(0xffff - (b & 0xffff)) : holder(b, -1, l);
-                if (l == r % G) { e[r / G] = x; k[r / G] = b; }
+        for (int i = 0; i < SLOTS; ++i) {
+            uint32_t mine = 0;
+            const int rounds = min(K - i * G, G);
+#pragma unroll 1
+            for (int r = 0; r < rounds; ++r) {
+                mine = l == r ? b : mine;
+                const uint32_t n = next(b);
+                if (!BF) close = close || ((b ^ n) & ~LOW) == 0;
+                b = n;
             }
+            e[i] = expert_of(mine);
         }
-        uint32_t bits = 0;
+        if constexpr (!BF) {
+            if (__any(close)) {                                // whole keys, equal ones by the expert
+                uint32_t last = ~0u;
+                int x = -1;
+                auto order = [&](int i, int j) { return order_of(p[i].get(j)); };
 #pragma unroll
-        for (int j = 0; j < 8; ++j) bits |= key[j] >= b ? 1u << j : 0u;
-        if constexpr (!PACKED) {
-            // equal logits among the picks: more than K keys reach the last, or the keys ran out
-            const int reach = (int)over_group<G>(__popc(bits), [](uint32_t p, uint32_t q) { return p + q; });
-            if (__any(reach != K || !falls)) {
-                b = best;
-                bits = 0;
-                int x = holder(b, -1, l);
-#pragma unroll
-                for (int r = 0; r < ROUNDS; ++r) {
+                for (int r = 0; r < ROUNDS; ++r)
                     if (r < K) {
-                        if (r) {
-                            const int same = holder(b, x, l);
-                            const uint32_t n = next(b);
-                            const int other = holder(n, -1, l);
-                            if (same < 8 * G) x = same;
-                            else { b = n; x = other; }
-                        }
-                        if (l == r % G) { e[r / G] = x; k[r / G] = b; }
-                        if (x / 8 == l) bits |= 1u << x % 8;
+                        auto behind = [&](int i, int j) {
+                            const uint32_t o = order(i, j);
+                            return real(i, j) && (r == 0 || o < last || (o == last && expert(i, j) > x));
+                        };
+                        const uint32_t o = over([&](int i, int j) { return behind(i, j) ? order(i, j) : 0u; }, umax);
+                        x = (int)over([&](int i, int j) { return behind(i, j) && order(i, j) == o ? (uint32_t)expert(i, j) : 1u << 20; }, umin);
+                        last = o;
+                        if (l == r % G) e[r / G] = x;
                     }
-                }
             }
         }
-        return bits;
     }
 };
 
@@ -135,30 +147,39 @@ __device__ __forceinline__ void balance_finish(float p, int c, int64_t grp, int 
     if (e == 0) loss[grp] = (float)(E * l);
 }
 
+// Threads of the largest block: more experts to a lane take more registers.
+constexpr int balance_most(int NP) { return NP > 2 ? 512 : 1024; }
+
 // A block walks its slice of a group's tokens; part (groups, slices, E): {sum of probabilities, count}.  With one slice to a
 // group the block has all of it and finishes the loss itself.
-template <typename T, int G, bool TAIL>
-__global__ void __launch_bounds__(RT_MOST)
+template <typename T, int NP, int G, bool FULL>
+__global__ void __launch_bounds__(balance_most(NP))
 balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, int32_t *__restrict__ topk_idx,
                float *__restrict__ topk_w, float2 *__restrict__ part, int64_t tokens, int slices, int E, int K,
                int32_t *__restrict__ counts, float *__restrict__ prob_mean, float *__restrict__ loss)
 {
-    __shared__ float psum[RT_MOST / 64][8 * G];
-    __shared__ int csum[RT_MOST / 64][8 * G];
+    typedef Token<T, NP, G, FULL> Tok;
+    __shared__ float psum[balance_most(NP) / 64][Tok::SIZE];
+    __shared__ int csum[Tok::SIZE];
     __shared__ double fin[2][4];
     const int64_t grp = blockIdx.x / slices;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane % G, at = lane / G;
     const int64_t stride = (int64_t)slices * (blockDim.x / G);
     const T *const z = logits + grp * tokens * E;
-    float acc[8] = {};
-    int cnt[8] = {};
+    if (threadIdx.x < Tok::SIZE) csum[threadIdx.x] = 0;
+    __syncthreads();
+    float acc[NP][8] = {};
     struct Step {
-        Piece<T, 8> p;
+        Piece<T, 8> p[NP];
         uint8_t on;
     };
     auto fetch = [&](Step &s, int64_t t) __attribute__((always_inline)) {        // t: first token of the wave
         const bool in = t + at < tokens;
-        s.p.template load<TAIL>(z + t * E + (uint32_t)(at * E + 8 * l), in ? E - 8 * l : 0);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int e = 8 * (l + G * i);
+            s.p[i].template load<!FULL>(z + t * E + (uint32_t)(at * E + e), in ? E - e : 0);
+        }
         s.on = in && (!mask || mask[grp * tokens + t + at]);
     };
     int64_t t = (int64_t)(blockIdx.x % slices) * (blockDim.x / G) + wave * (64 / G);
@@ -167,63 +188,67 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
     for (; t < tokens; t += stride) {
         const Step s = next;
         if (t + stride < tokens) fetch(next, t + stride);
-        Token<T, G> tok;
-        tok.take(s.p, l, E);
-        const uint32_t best = tok.first();
-        int e[Token<T, G>::SLOTS];
-        uint32_t k[Token<T, G>::SLOTS];
-        const uint32_t bits = tok.picks(best, K, l, e, k);
-        const float m = tok.value(best);
+        const Tok tok(s.p, l, E);
+        int e[Tok::SLOTS];
+        tok.picks(K, e);
+        const float m = tok.top;
         bool on = s.on;
-        if (__any(m == -INFINITY)) {                           // a token without a logit above it counts nothing
-            uint32_t some = 0;
+        if (__any(m == -INFINITY)) {                           // a token whose logits are all -inf does not count
+            uint32_t other = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) some |= 8 * l + j < E && tok.f[j] != -INFINITY;
-            on = on && over_group<G>(some, [](uint32_t a, uint32_t b) { return a | b; });
-        }
-        float p[8], Z = 0.f;
+            for (int i = 0; i < NP; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            p[j] = 8 * l + j < E ? route_exp(tok.f[j] - m) : 0.f;
-            Z += p[j];
+                for (int j = 0; j < 8; ++j) other |= tok.real(i, j) && s.p[i].get(j) != -INFINITY;
+            on = on && over_group<G>(other, umax);
         }
+        float p[NP][8], Z = 0.f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                p[i][j] = tok.real(i, j) ? route_exp(s.p[i].get(j) - m) : 0.f;
+                Z += p[i][j];
+            }
         const float invZ = 1.0f / group_sum<G>(Z);
         if (t + at < tokens) {
-            const int64_t row = (grp * tokens + t + at) * K;
+            const int64_t row = grp * tokens + t + at;
 #pragma unroll
-            for (int i = 0; i < Token<T, G>::SLOTS; ++i) {
+            for (int i = 0; i < Tok::SLOTS; ++i) {
                 const int r = i * G + l;
                 if (r < K) {
-                    if (topk_idx) topk_idx[row + r] = e[i];
-                    if (topk_w) topk_w[row + r] = route_exp(tok.value(k[i]) - m) * invZ;
+                    if (topk_idx) topk_idx[row * K + r] = e[i];
+                    if (topk_w) topk_w[row * K + r] = route_exp(to_float(logits[row * E + e[i]]) - m) * invZ;
+                    if (on) atomicAdd(&csum[e[i]], 1);         // whole numbers: the order does not matter
                 }
             }
         }
         if (on) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                acc[j] += p[j] * invZ;
-                cnt[j] += bits >> j & 1;
-            }
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[i][j] += p[i][j] * invZ;
         }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float v = __uint_as_float(over_lanes<G, 64>(__float_as_uint(acc[j]), add_f32));
-        const int c = (int)over_lanes<G, 64>((uint32_t)cnt[j], [](uint32_t a, uint32_t b) { return a + b; });
-        if (lane < G) { psum[wave][8 * l + j] = v; csum[wave][8 * l + j] = c; }
-    }
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float v = __uint_as_float(over_lanes<G, 64>(__float_as_uint(acc[i][j]), add_f32));
+            if (lane < G) psum[wave][8 * (l + G * i) + j] = v;
+        }
     __syncthreads();
     const int x = threadIdx.x;
     float v = 0.f;
     int c = 0;
-    if (x < E)
-        for (int w = 0; w < (int)blockDim.x / 64; ++w) { v += psum[w][x]; c += csum[w][x]; }
+    if (x < E) {
+        c = csum[x];
+        for (int w = 0; w < (int)blockDim.x / 64; ++w) v += psum[w][x];
+    }
     if (slices == 1) balance_finish(v, c, grp, E, K, counts, prob_mean, loss, fin);
     else if (x < E) part[(int64_t)blockIdx.x * E + x] = make_float2(v, __int_as_float(c));
 }
 
-// the slices joined, each thread every (1024 / width)-th of an expert
+// The slices joined, each thread every (1024 / width)-th of an expert, 16 of them under way.
 __global__ void __launch_bounds__(1024)
 balance_loss_kernel(const float2 *__restrict__ part, int slices, int width, int E, int K, int32_t *__restrict__ counts,
                     float *__restrict__ prob_mean, float *__restrict__ loss)
@@ -235,7 +260,7 @@ balance_loss_kernel(const float2 *__restrict__ part, int slices, int width, int 
     int c = 0;
     float p = 0.f;
     if (e < E) {
-#pragma unroll 8
+#pragma unroll 16
         for (int s = threadIdx.x / width; s < slices; s += n) {
             const float2 v = part[(grp * slices + s) * E + e];
             p += v.x;
@@ -256,36 +281,44 @@ balance_loss_kernel(const float2 *__restrict__ part, int slices, int width, int 
 
 namespace {
 
-int lanes_of(int E)                        // of a token
+int power_of_two(int n)
 {
-    int g = 1;
-    while (8 * g < E) g *= 2;
-    return g;
+    int p = 1;
+    while (p < n) p *= 2;
+    return p;
 }
+int lanes_of(int E) { return power_of_two((E + 7) / 8); }      // of a token, eight experts to a lane
+// Eight lanes at most for the routing: steps over lanes cost as much as three experts of a lane, and with few tokens to a wave
+// so does what is done once for all of them.
+int pieces_of(int E) { return E <= 64 ? 1 : E <= 128 ? 2 : 4; }
+int routing_lanes_of(int E) { return E <= 64 ? lanes_of(E) : 8; }
 
-// Threads of a block and slices of a group.  A group that a block of 1024 threads walks in four steps or less stays with one
-// block, without a second launch; beyond, a slice is a step or more, and the slices of all groups are some 256 (a few more
-// where groups are many), which fill the chip with waves and are soon added up.
+// Threads of a block and slices of a group.  A group that a block walks in four steps or less stays with one block, without a
+// second launch; beyond, a slice is a step or more, and the slices of all groups are some 256 (a few more where groups are
+// many), which fill the chip with waves and are soon added up.
 struct Slices { int threads; int64_t count; };
 Slices balance_slices(int64_t groups, int64_t tokens, int E)
 {
-    const int64_t threads = tokens * lanes_of(E), steps = (threads + RT_MOST - 1) / RT_MOST;
+    const int most = balance_most(pieces_of(E));
+    const int64_t threads = tokens * routing_lanes_of(E), steps = (threads + most - 1) / most;
     if (steps <= 4 || groups >= 256) {
         int n = 256;
-        while (n < RT_MOST && n < threads) n *= 2;
+        while (n < most && n < threads) n *= 2;
         return {n, 1};
     }
-    const int64_t most = 256 / groups + 1;
-    return {RT_MOST, steps < most ? steps : most};
+    const int64_t slices = 1024 / most * 256 / groups + 1;
+    return {most, steps < slices ? steps : slices};
 }
 
+// f(lanes, whether the last piece is short, whether the experts fill the lanes) as constants
 template <typename F>
 void with_lanes(int E, F &&f)
 {
     using std::integral_constant;
     auto tail = [&](auto g) {
-        if (E % 8) f(g, std::true_type());
-        else f(g, std::false_type());
+        if (E % 8) f(g, std::true_type(), std::false_type());
+        else if (E < 8 * g) f(g, std::false_type(), std::false_type());
+        else f(g, std::false_type(), std::true_type());
     };
     switch (lanes_of(E)) {
     case 1: return tail(integral_constant<int, 1>());
@@ -311,19 +344,18 @@ swimba_status launch_router_balance(int64_t groups, int64_t tokens, int E, int K
 {
     if (groups == 0) return SWIMBA_OK;
     const Slices s = balance_slices(groups, tokens, E);
-    with_lanes(E, [&](auto g, auto tail) {
+    with_lanes(E, [&](auto lanes, auto, auto full) {
+        constexpr int G = lanes() < 8 ? lanes() : 8, NP = lanes() / G;
         auto go = [&](auto kernel, auto *z) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * s.count)), dim3(s.threads), 0, st, z, mask, topk_idx, topk_w, (float2 *)part,
                                tokens, (int)s.count, E, K, counts, prob_mean, loss);
         };
-        if (io_dtype == SWIMBA_BF16) go(balance_kernel<bf16, g(), tail()>, (const bf16 *)logits);
-        else go(balance_kernel<float, g(), tail()>, (const float *)logits);
+        if (io_dtype == SWIMBA_BF16) go(balance_kernel<bf16, NP, G, full()>, (const bf16 *)logits);
+        else go(balance_kernel<float, NP, G, full()>, (const float *)logits);
     });
     SWIMBA_CHECK_LAUNCH();
     if (s.count > 1) {
-        int width = 1;
-        while (width < E) width *= 2;
-        hipLaunchKernelGGL(balance_loss_kernel, dim3((unsigned)groups), dim3(1024), 0, st, (const float2 *)part, (int)s.count, width, E, K,
+        hipLaunchKernelGGL(balance_loss_kernel, dim3((unsigned)groups), dim3(1024), 0, st, (const float2 *)part, (int)s.count, power_of_two(E), E, K,
                            counts, prob_mean, loss);
         SWIMBA_CHECK_LAUNCH();
     }
@@ -338,7 +370,7 @@ router_bwd_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask
                   const float *__restrict__ d_topk_w, const int32_t *__restrict__ counts, const float *__restrict__ d_loss,
                   T *__restrict__ d_logits, int64_t tokens, int64_t per_group, int E, int K)
 {
-    constexpr int SLOTS = Token<T, G>::SLOTS;
+    constexpr int SLOTS = Token<T, 1, G, true>::SLOTS;
     __shared__ float lds[4][512];
     const int64_t grp = blockIdx.x / per_group;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane % G, at = lane / G;
@@ -415,10 +447,8 @@ router_bwd_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask
             m = fmaxf(m, f[j]);
             any |= f[j] != -INFINITY;
         }
-        m = __uint_as_float(over_group<G>(__float_as_uint(m), [](uint32_t a, uint32_t b) {
-            return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
-        }));
-        const uint32_t both = over_group<G>(any | some << 1, [](uint32_t a, uint32_t b) { return a | b; });
+        m = __uint_as_float(over_group<G>(__float_as_uint(m), max_f32));
+        const uint32_t both = over_group<G>(any | some << 1, or_u32);
         float p[8], Z = 0.f, dot = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -440,7 +470,7 @@ swimba_status launch_router_bwd(int64_t groups, int64_t tokens, int E, int K, in
 {
     if (groups == 0 || tokens == 0) return SWIMBA_OK;
     const int64_t need = (tokens * lanes_of(E) + 255) / 256, fit = groups < 2048 ? 2048 / groups : 1, per_group = need < fit ? need : fit;
-    with_lanes(E, [&](auto g, auto tail) {
+    with_lanes(E, [&](auto g, auto tail, auto) {
         auto go = [&](auto kernel, auto *z, auto *out) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * per_group)), dim3(256), 0, st, z, mask, topk_idx, d_topk_w, counts, d_loss, out,
                                tokens, per_group, E, K);
