@@ -8,31 +8,39 @@
 
 namespace swimba {
 
-// Order of 16-bit pairs of bf16 bits as unsigned numbers: -0 as +0, NaN outside the numbers by sign.
-__device__ __forceinline__ uint32_t order_of_pair(uint32_t u)
+// Place of a logit among all: smaller the larger it is, -0 as +0, NaN outside the numbers by sign.  Of two bf16 at once,
+// as 16-bit numbers, and of a float.
+__device__ __forceinline__ uint32_t place_of_pair(uint32_t u)
 {
+    typedef uint16_t __attribute__((ext_vector_type(2))) u16x2;
     typedef int16_t __attribute__((ext_vector_type(2))) s16x2;
     const uint32_t neg = __builtin_bit_cast(uint32_t, __builtin_bit_cast(s16x2, u) >> (int16_t)15);
-    const uint32_t add = (neg & 0x80018001u) ^ 0x80008000u;            // positive u: u + 2^15; negative: ~u + 1
-    return __builtin_bit_cast(uint32_t, (s16x2)(__builtin_bit_cast(s16x2, u ^ neg) + __builtin_bit_cast(s16x2, add)));
+    const uint32_t from = (neg & 0x80018001u) ^ 0x7fff7fffu;           // positive u: 2^15 - 1 - u; negative: -2 - ~u
+    return __builtin_bit_cast(uint32_t, (u16x2)(__builtin_bit_cast(u16x2, from) - __builtin_bit_cast(u16x2, u ^ neg)));
 }
-__device__ __forceinline__ uint32_t order_of(float f)
+__device__ __forceinline__ float at_place(uint32_t place)              // of a bf16, in the lower half
+{
+    const uint32_t s = ~place;
+    return __uint_as_float((s & 0x8000u ? s ^ 0x8000u : 0u - s) << 16);
+}
+__device__ __forceinline__ uint32_t place_of(float f)
 {
     const uint32_t u = __float_as_uint(f + 0.0f);
-    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return u ^ (~(uint32_t)((int32_t)u >> 31) & 0x7fffffffu);
 }
+__device__ __forceinline__ float at_whole_place(uint32_t place) { return __uint_as_float(place & 0x80000000u ? place : place ^ 0x7fffffffu); }
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint32_t umin(uint32_t a, uint32_t b) { return a < b ? a : b; }
 
 // One token in G lanes, 8 NP experts to a lane: piece i of lane l are the experts from 8 (l + G i) on.
-// A key is larger the earlier its expert is picked, and 0 past the last expert.  Its lowest bits are the expert's, counted
-// down, so that all keys differ and name their experts; above them lie all 16 bits of a bf16 logit's order, or the upper 24 of
-// an fp32 one's, which do not decide between logits that agree that far: those are picked by the whole of them (`close`).
-// FULL: the experts fill the lanes.
+// A key is smaller the earlier its expert is picked.  Its lowest bits are the expert's number, so that all keys differ and
+// name their experts; above them lies the place of a bf16 logit, or the upper 24 bits of an fp32 one's, which do not decide
+// between logits that agree that far: those are picked by the whole of them (`close`).  The lane's part of the number, 8 l,
+// is not in the stored keys: it is added to what a lane has found.  FULL: the experts fill the lanes.
 template <typename T, int NP, int G, bool FULL> struct Token {
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr int SIZE = 8 * NP * G, ROUNDS = SIZE < SWIMBA_MAX_TOPK ? SIZE : SWIMBA_MAX_TOPK, SLOTS = (ROUNDS + G - 1) / G;
-    static constexpr uint32_t LOW = BF ? 0xffffu : 0xffu;
+    static constexpr uint32_t LOW = BF ? 0xffffu : 0xffu, NONE = ~0u;
     const Piece<T, 8> (&p)[NP];
     const int l, E;
     uint32_t key[NP][8], best;
@@ -42,47 +50,43 @@ template <typename T, int NP, int G, bool FULL> struct Token {
     __device__ __forceinline__ bool real(int i, int j) const { return FULL || expert(i, j) < E; }
     __device__ __forceinline__ Token(const Piece<T, 8> (&pieces)[NP], int lane, int experts) : p(pieces), l(lane), E(experts)
     {
-        uint32_t most = 0;
+        uint32_t whole = NONE;
 #pragma unroll
         for (int i = 0; i < NP; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const uint32_t low = LOW - expert(i, j);
+                const uint32_t low = 8 * G * i + j;
                 uint32_t k;
                 if constexpr (BF) {
-                    const uint32_t s = order_of_pair(p[i].v[j / 2]);
+                    const uint32_t s = place_of_pair(p[i].v[j / 2]);
                     k = j % 2 ? (s & 0xffff0000u) | low : s << 16 | low;
                 } else {
-                    const uint32_t s = order_of(p[i].get(j));
-                    most = umax(most, real(i, j) ? s : 0);
+                    const uint32_t s = place_of(p[i].get(j));
+                    whole = umin(whole, real(i, j) ? s : NONE);
                     k = (s & ~LOW) | low;
                 }
-                key[i][j] = real(i, j) ? k : 0;
+                key[i][j] = real(i, j) ? k : NONE - 8 * l;
+                asm("" : "+v"(key[i][j]));                     // the whole key: taken apart, it would cost every pick an addition
             }
-        best = over([&](int i, int j) { return key[i][j]; }, umax);
-        if constexpr (BF) {
-            const uint32_t s = best >> 16;
-            top = __uint_as_float((s & 0x8000u ? s ^ 0x8000u : 0u - s) << 16);
-        } else {
-            most = over_group<G>(most, umax);
-            top = __uint_as_float(most & 0x80000000u ? most ^ 0x80000000u : ~most);
-        }
+        best = over([&](int i, int j) { return key[i][j]; }, umin, 8 * l);
+        top = BF ? at_place(best >> 16) : at_whole_place(over_group<G>(whole, umin));
     }
-    template <typename F> __device__ __forceinline__ uint32_t over(F f, uint32_t (*op)(uint32_t, uint32_t)) const
+    // op over the lanes of f over the lane's experts, with `more` added in each lane
+    template <typename F> __device__ __forceinline__ uint32_t over(F f, uint32_t (*op)(uint32_t, uint32_t), uint32_t more = 0) const
     {
         uint32_t v = f(0, 0);
 #pragma unroll
         for (int i = 0; i < NP; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v = op(v, f(i, j));
-        return over_group<G>(v, op);
+        return over_group<G>(v + more, op);
     }
-    // largest key below `best`: at the smallest distance under it, those at and above it being far away
-    __device__ __forceinline__ uint32_t next(uint32_t best) const
+    // smallest key above `last`: at the smallest distance over it, those at and below it being far away
+    __device__ __forceinline__ uint32_t next(uint32_t last) const
     {
-        return best - 1 - over([&](int i, int j) { return best - 1 - key[i][j]; }, umin);
+        const uint32_t from = last + 1 - 8 * l;
+        return last + 1 + over([&](int i, int j) { return key[i][j] - from; }, umin);
     }
-    static __device__ __forceinline__ int expert_of(uint32_t k) { return (int)(LOW - (k & LOW)); }
 
     // The K picks: lane l keeps the experts of rounds l, l + G, ...
     __device__ __forceinline__ void picks(int K, int (&e)[SLOTS]) const
@@ -100,25 +104,28 @@ template <typename T, int NP, int G, bool FULL> struct Token {
                 if (!BF) close = close || ((b ^ n) & ~LOW) == 0;
                 b = n;
             }
-            e[i] = expert_of(mine);
+            e[i] = mine & LOW;
         }
         if constexpr (!BF) {
-            if (__any(close)) {                                // whole keys, equal ones by the expert
-                uint32_t last = ~0u;
+            if (__any(close)) {                                // whole places, equal ones by the expert
+                uint32_t last = 0;
                 int x = -1;
-                auto order = [&](int i, int j) { return order_of(p[i].get(j)); };
+                auto place = [&](int i, int j) { return place_of(p[i].get(j)); };
 #pragma unroll
-                for (int r = 0; r < ROUNDS; ++r)
-                    if (r < K) {
-                        auto behind = [&](int i, int j) {
-                            const uint32_t o = order(i, j);
-                            return real(i, j) && (r == 0 || o < last || (o == last && expert(i, j) > x));
+                for (int i = 0; i < SLOTS; ++i) {
+                    const int rounds = min(K - i * G, G);
+#pragma unroll 1
+                    for (int r = 0; r < rounds; ++r) {
+                        auto behind = [&](int q, int j) {
+                            const uint32_t o = place(q, j);
+                            return real(q, j) && (o > last || (o == last && expert(q, j) > x));
                         };
-                        const uint32_t o = over([&](int i, int j) { return behind(i, j) ? order(i, j) : 0u; }, umax);
-                        x = (int)over([&](int i, int j) { return behind(i, j) && order(i, j) == o ? (uint32_t)expert(i, j) : 1u << 20; }, umin);
+                        const uint32_t o = over([&](int q, int j) { return behind(q, j) ? place(q, j) : NONE; }, umin);
+                        x = (int)over([&](int q, int j) { return behind(q, j) && place(q, j) == o ? (uint32_t)expert(q, j) : 1u << 20; }, umin);
                         last = o;
-                        if (l == r % G) e[r / G] = x;
+                        e[i] = l == r ? x : e[i];
                     }
+                }
             }
         }
     }
@@ -147,19 +154,19 @@ __device__ __forceinline__ void balance_finish(float p, int c, int64_t grp, int 
     if (e == 0) loss[grp] = (float)(E * l);
 }
 
-// Threads of the largest block: more experts to a lane take more registers.
-constexpr int balance_most(int NP) { return NP > 2 ? 512 : 1024; }
+// Threads of the largest block: 32 fp32 logits to a lane take the registers of two.
+constexpr int balance_most(int NP, int element) { return NP > 2 && element == 4 ? 512 : 1024; }
 
 // A block walks its slice of a group's tokens; part (groups, slices, E): {sum of probabilities, count}.  With one slice to a
 // group the block has all of it and finishes the loss itself.
 template <typename T, int NP, int G, bool FULL>
-__global__ void __launch_bounds__(balance_most(NP))
+__global__ void __launch_bounds__(balance_most(NP, sizeof(T)))
 balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, int32_t *__restrict__ topk_idx,
                float *__restrict__ topk_w, float2 *__restrict__ part, int64_t tokens, int slices, int E, int K,
-               int32_t *__restrict__ counts, float *__restrict__ prob_mean, float *__restrict__ loss)
+               int32_t *__restrict__ counts, float *__restrict__ prob_mean, float *__restrict__ loss, int *__restrict__ ticket)
 {
     typedef Token<T, NP, G, FULL> Tok;
-    __shared__ float psum[balance_most(NP) / 64][Tok::SIZE];
+    __shared__ float psum[balance_most(NP, sizeof(T)) / 64][Tok::SIZE];
     __shared__ int csum[Tok::SIZE];
     __shared__ double fin[2][4];
     const int64_t grp = blockIdx.x / slices;
@@ -167,6 +174,7 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
     const int64_t stride = (int64_t)slices * (blockDim.x / G);
     const T *const z = logits + grp * tokens * E;
     if (threadIdx.x < Tok::SIZE) csum[threadIdx.x] = 0;
+    if (slices > 1 && threadIdx.x == 0 && blockIdx.x % slices == 0) ticket[grp] = 0;
     __syncthreads();
     float acc[NP][8] = {};
     struct Step {
@@ -183,11 +191,16 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
         s.on = in && (!mask || mask[grp * tokens + t + at]);
     };
     int64_t t = (int64_t)(blockIdx.x % slices) * (blockDim.x / G) + wave * (64 / G);
+    constexpr bool AHEAD = NP < 4;                             // with more experts to a lane, its registers serve another wave better
     Step next;
-    if (t < tokens) fetch(next, t);
+    if (AHEAD && t < tokens) fetch(next, t);
     for (; t < tokens; t += stride) {
-        const Step s = next;
-        if (t + stride < tokens) fetch(next, t + stride);
+        Step s;
+        if constexpr (AHEAD) {
+            s = next;
+            if (t + stride < tokens) fetch(next, t + stride);
+        } else
+            fetch(s, t);
         const Tok tok(s.p, l, E);
         int e[Tok::SLOTS];
         tok.picks(K, e);
@@ -248,34 +261,54 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
     else if (x < E) part[(int64_t)blockIdx.x * E + x] = make_float2(v, __int_as_float(c));
 }
 
-// The slices joined, each thread every (1024 / width)-th of an expert, 16 of them under way.
+// The slices of a group joined, 32 experts to a block of 1024 threads: 32 half waves take every 32nd slice each.  The block that
+// is done last (a ticket that balance_kernel has set to zero) finishes the loss; what it adds up has an order of its own, so
+// that it does not matter which one that is.
 __global__ void __launch_bounds__(1024)
-balance_loss_kernel(const float2 *__restrict__ part, int slices, int width, int E, int K, int32_t *__restrict__ counts,
-                    float *__restrict__ prob_mean, float *__restrict__ loss)
+balance_loss_kernel(const float2 *__restrict__ part, int slices, int E, int K, int32_t *counts, float *__restrict__ prob_mean,
+                    float *__restrict__ loss, float *psums, int *ticket)
 {
-    __shared__ float2 lds[1024];
+    __shared__ float2 lds[32][33];
     __shared__ double fin[2][4];
-    const int64_t grp = blockIdx.x;
-    const int e = threadIdx.x % width, n = 1024 / width;
+    __shared__ bool last;
+    const int blocks = (E + 31) / 32;
+    const int64_t grp = blockIdx.x / blocks;
+    const int col = threadIdx.x % 32, row = threadIdx.x / 32, e = blockIdx.x % blocks * 32 + col;
     int c = 0;
     float p = 0.f;
     if (e < E) {
-#pragma unroll 16
-        for (int s = threadIdx.x / width; s < slices; s += n) {
+#pragma unroll 8
+        for (int s = row; s < slices; s += 32) {
             const float2 v = part[(grp * slices + s) * E + e];
             p += v.x;
             c += __float_as_int(v.y);
         }
     }
-    lds[threadIdx.x] = make_float2(p, __int_as_float(c));
+    lds[row][col] = make_float2(p, __int_as_float(c));
     __syncthreads();
     p = 0.f;
     c = 0;
-    if (threadIdx.x < width)
-        for (int i = 0; i < n; ++i) {
-            p += lds[i * width + e].x;
-            c += __float_as_int(lds[i * width + e].y);
+    if (row == 0)
+        for (int i = 0; i < 32; ++i) {
+            p += lds[i][col].x;
+            c += __float_as_int(lds[i][col].y);
         }
+    if (blocks > 1) {
+        if (row == 0 && e < E) {
+            __hip_atomic_store(psums + grp * E + e, p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(counts + grp * E + e, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) last = __hip_atomic_fetch_add(ticket + grp, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
+        __syncthreads();
+        if (!last) return;
+        __threadfence();
+        const int x = threadIdx.x;
+        if (x < E) {
+            p = __hip_atomic_load(psums + grp * E + x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            c = __hip_atomic_load(counts + grp * E + x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
     balance_finish(p, c, grp, E, K, counts, prob_mean, loss, fin);
 }
 
@@ -297,9 +330,9 @@ int routing_lanes_of(int E) { return E <= 64 ? lanes_of(E) : 8; }
 // second launch; beyond, a slice is a step or more, and the slices of all groups are some 256 (a few more where groups are
 // many), which fill the chip with waves and are soon added up.
 struct Slices { int threads; int64_t count; };
-Slices balance_slices(int64_t groups, int64_t tokens, int E)
+Slices balance_slices(int64_t groups, int64_t tokens, int E, int element)
 {
-    const int most = balance_most(pieces_of(E));
+    const int most = balance_most(pieces_of(E), element);
     const int64_t threads = tokens * routing_lanes_of(E), steps = (threads + most - 1) / most;
     if (steps <= 4 || groups >= 256) {
         int n = 256;
@@ -332,31 +365,36 @@ void with_lanes(int E, F &&f)
 
 }  // namespace
 
+// scratch of the sums in slices: part, then the joined sums of the probabilities and a ticket for each group
+// (for the type that takes more slices)
 size_t balance_bytes(int64_t groups, int64_t tokens, int E)
 {
-    const int64_t n = balance_slices(groups, tokens, E).count;
-    return n > 1 ? (size_t)groups * n * E * sizeof(float2) : 0;
+    const int64_t a = balance_slices(groups, tokens, E, 2).count, b = balance_slices(groups, tokens, E, 4).count, n = a > b ? a : b;
+    return n > 1 ? (size_t)groups * (n * E * sizeof(float2) + E * sizeof(float) + sizeof(int)) : 0;
 }
 
 swimba_status launch_router_balance(int64_t groups, int64_t tokens, int E, int K, int io_dtype, const void *logits,
                                     const uint8_t *mask, int32_t *topk_idx, float *topk_w, int32_t *counts, float *prob_mean,
-                                    float *loss, void *part, hipStream_t st)
+                                    float *loss, void *work, hipStream_t st)
 {
     if (groups == 0) return SWIMBA_OK;
-    const Slices s = balance_slices(groups, tokens, E);
+    const Slices s = balance_slices(groups, tokens, E, io_dtype == SWIMBA_BF16 ? 2 : 4);
+    float2 *const part = (float2 *)work;
+    float *const psums = (float *)(part + groups * s.count * E);
+    int *const ticket = (int *)(psums + groups * E);
     with_lanes(E, [&](auto lanes, auto, auto full) {
         constexpr int G = lanes() < 8 ? lanes() : 8, NP = lanes() / G;
         auto go = [&](auto kernel, auto *z) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * s.count)), dim3(s.threads), 0, st, z, mask, topk_idx, topk_w, (float2 *)part,
-                               tokens, (int)s.count, E, K, counts, prob_mean, loss);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * s.count)), dim3(s.threads), 0, st, z, mask, topk_idx, topk_w, part, tokens,
+                               (int)s.count, E, K, counts, prob_mean, loss, ticket);
         };
         if (io_dtype == SWIMBA_BF16) go(balance_kernel<bf16, NP, G, full()>, (const bf16 *)logits);
         else go(balance_kernel<float, NP, G, full()>, (const float *)logits);
     });
     SWIMBA_CHECK_LAUNCH();
     if (s.count > 1) {
-        hipLaunchKernelGGL(balance_loss_kernel, dim3((unsigned)groups), dim3(1024), 0, st, (const float2 *)part, (int)s.count, power_of_two(E), E, K,
-                           counts, prob_mean, loss);
+        hipLaunchKernelGGL(balance_loss_kernel, dim3((unsigned)(groups * ((E + 31) / 32))), dim3(1024), 0, st, part, (int)s.count, E, K,
+                           counts, prob_mean, loss, psums, ticket);
         SWIMBA_CHECK_LAUNCH();
     }
     return SWIMBA_OK;
