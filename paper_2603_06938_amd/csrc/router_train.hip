@@ -100,6 +100,7 @@ template <typename T, int NP, int G, bool FULL> struct Token {
 #pragma unroll 1
             for (int r = 0; r < rounds; ++r) {
                 mine = l == r ? b : mine;
+                if (BF && i * G + r == K - 1) break;           // the pick behind the last shows whether fp32 ones are close
                 const uint32_t n = next(b);
                 if (!BF) close = close || ((b ^ n) & ~LOW) == 0;
                 b = n;
@@ -214,14 +215,25 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
                 for (int j = 0; j < 8; ++j) other |= tok.real(i, j) && s.p[i].get(j) != -INFINITY;
             on = on && over_group<G>(other, umax);
         }
+        // exp(f - m) as exp2(f c - m c) in one rounding; m c, and with it the weights, would overflow for the largest of numbers
         float p[NP][8], Z = 0.f;
+        const float mc = m * LOG2E;
+        const bool far = __any(fabsf(m) > 2e38f);
 #pragma unroll
         for (int i = 0; i < NP; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                p[i][j] = tok.real(i, j) ? route_exp(s.p[i].get(j) - m) : 0.f;
-                Z += p[i][j];
-            }
+            for (int j = 0; j < 8; ++j)
+                p[i][j] = tok.real(i, j) ? fast_exp2(fmaf(s.p[i].get(j), LOG2E, -mc)) : 0.f;
+        if (far) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[i][j] = tok.real(i, j) ? route_exp(s.p[i].get(j) - m) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) Z += p[i][j];
         const float invZ = 1.0f / group_sum<G>(Z);
         if (t + at < tokens) {
             const int64_t row = grp * tokens + t + at;
@@ -242,13 +254,14 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
                 for (int j = 0; j < 8; ++j) acc[i][j] += p[i][j] * invZ;
         }
     }
+    float sum[8 * NP];
+    int first = 0;
 #pragma unroll
-    for (int i = 0; i < NP; ++i)
+    for (int i = 0; i < 8 * NP; ++i) sum[i] = acc[i / 8][i % 8];
+    sum_over<32, G>(sum, first, lane);
+    constexpr int LEFT = NP * G > 8 ? NP * G / 8 : 1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float v = __uint_as_float(over_lanes<G, 64>(__float_as_uint(acc[i][j]), add_f32));
-            if (lane < G) psum[wave][8 * (l + G * i) + j] = v;
-        }
+    for (int i = 0; i < LEFT; ++i) psum[wave][8 * (l + G * ((first + i) / 8)) + (first + i) % 8] = sum[i];  // one from several lanes: the same
     __syncthreads();
     const int x = threadIdx.x;
     float v = 0.f;
@@ -323,8 +336,9 @@ int power_of_two(int n)
 int lanes_of(int E) { return power_of_two((E + 7) / 8); }      // of a token, eight experts to a lane
 // Eight lanes at most for the routing: steps over lanes cost as much as three experts of a lane, and with few tokens to a wave
 // so does what is done once for all of them.
-int pieces_of(int E) { return E <= 64 ? 1 : E <= 128 ? 2 : 4; }
-int routing_lanes_of(int E) { return E <= 64 ? lanes_of(E) : 8; }
+constexpr int pieces_for(int lanes) { return lanes <= 4 ? 1 : lanes <= 8 ? 2 : 4; }
+int pieces_of(int E) { return pieces_for(lanes_of(E)); }
+int routing_lanes_of(int E) { return lanes_of(E) / pieces_of(E); }
 
 // Threads of a block and slices of a group.  A group that a block walks in four steps or less stays with one block, without a
 // second launch; beyond, a slice is a step or more, and the slices of all groups are some 256 (a few more where groups are
@@ -383,7 +397,7 @@ swimba_status launch_router_balance(int64_t groups, int64_t tokens, int E, int K
     float *const psums = (float *)(part + groups * s.count * E);
     int *const ticket = (int *)(psums + groups * E);
     with_lanes(E, [&](auto lanes, auto, auto full) {
-        constexpr int G = lanes() < 8 ? lanes() : 8, NP = lanes() / G;
+        constexpr int NP = pieces_for(lanes()), G = lanes() / NP;
         auto go = [&](auto kernel, auto *z) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * s.count)), dim3(s.threads), 0, st, z, mask, topk_idx, topk_w, part, tokens,
                                (int)s.count, E, K, counts, prob_mean, loss, ticket);

@@ -139,6 +139,37 @@ __device__ __forceinline__ uint32_t max_f32(uint32_t a, uint32_t b) { return __f
 __device__ __forceinline__ uint32_t or_u32(uint32_t a, uint32_t b) { return a | b; }
 template <int G> __device__ __forceinline__ float group_sum(float v) { return __uint_as_float(over_group<G>(__float_as_uint(v), add_f32)); }
 
+// Sums of N values over the lanes whose numbers differ in the bits from G to below 2 D.  While a lane has several, a step halves
+// them: the lanes with bit D clear keep the lower half, the others the upper.  v[i] is then the sum of value `first` + i.
+template <int D, int G, int N, int LEFT = N>
+__device__ __forceinline__ void sum_over(float (&v)[N], int &first, int lane)
+{
+    if constexpr (D >= G) {
+        if constexpr (LEFT > 1) {
+#pragma unroll
+            for (int i = 0; i < LEFT / 2; ++i) {
+                uint32_t a = __float_as_uint(v[i]), b = __float_as_uint(v[i + LEFT / 2]);
+                if constexpr (D >= 16) {
+                    const auto r = D == 16 ? __builtin_amdgcn_permlane16_swap(a, b, false, false) : __builtin_amdgcn_permlane32_swap(a, b, false, false);
+                    v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+                } else {
+                    const bool hi = lane & D;
+                    const uint32_t keep = hi ? b : a, send = hi ? a : b;
+                    uint32_t got;
+                    if constexpr (D == 4) got = (uint32_t)__builtin_amdgcn_ds_swizzle((int)send, 0x101f);
+                    else got = partner<D>(send);
+                    v[i] = __uint_as_float(keep) + __uint_as_float(got);
+                }
+            }
+            first += lane & D ? LEFT / 2 : 0;
+            sum_over<D / 2, G, N, LEFT / 2>(v, first, lane);
+        } else {
+            v[0] = __uint_as_float(over_lanes<D, 2 * D>(__float_as_uint(v[0]), add_f32));
+            sum_over<D / 2, G, N, 1>(v, first, lane);
+        }
+    }
+}
+
 // sum over the 64 lanes, in every lane
 __device__ __forceinline__ float wave_sum(float v) { return group_sum<64>(v); }
 
