@@ -1,10 +1,10 @@
 // Backward pass of the router's linear map:  du = dl W + du_add,  dW = dl^T u   (dl: gradient of the logits).
-// Bound by memory up to some hundred experts: u is read once, du written once.  Neither product goes through LDS: a wave owns
-// 128 columns, eight consecutive ones to a lane (16-byte pieces of the rows), and takes the operand of a 16 x 16 matrix
-// instruction out of eight rows by transposing 8 x 8 elements in registers; column n of tile i is then feature 8 n + i, so
-// that a lane's results are consecutive features as well.
-//   dW  k runs over the tokens: the wave keeps its sums (16 experts a tile) while it walks its tokens, 32 at a time; the sums
-//       of a block's waves are joined in LDS, those of the blocks by a second launch
+// Bound by memory up to some hundred experts in bf16, some sixty in fp32: u is read once, du written once.  Neither product
+// goes through LDS: a wave owns 128 columns, eight consecutive ones to a lane, and column n of tile i is feature 8 n + i, so
+// that operands come as whole pieces of rows and a lane's results are consecutive features as well.  A bf16 matrix
+// instruction wants eight rows of one column in a lane: 8 x 8 elements are transposed in registers.
+//   dW  k runs over the tokens: the wave keeps its sums (16 experts a tile) while it walks its tokens; the sums of a block's
+//       waves are joined in LDS, those of the blocks by a second launch
 //   du  k runs over the experts: W is kept in registers, 16 tokens at a time
 #include "rows.hpp"
 
@@ -21,6 +21,12 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t even, uint32_t odd, int i)
     return __builtin_amdgcn_perm(odd, even, i % 2 ? 0x07060302u : 0x05040100u);
 }
 
+__device__ __forceinline__ f32x4_t mfma4(uint32_t a, uint32_t b, f32x4_t c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a), __uint_as_float(b), c, 0, 0, 0);
+}
+
+template <typename T> constexpr int dw_step() { return sizeof(T) == 2 ? 32 : 16; }
 constexpr int LB_COLS = 128;           // features of a wave
 constexpr int LB_WAVES = 4;
 
@@ -32,33 +38,41 @@ struct Cols {
 };
 
 // dW: ME tiles of 16 experts, row m of tile j is expert e0 + ME m + j, so that a lane's experts are consecutive.
-template <int ME>
-__device__ __forceinline__ void dw_block(const bf16 *__restrict__ u, const bf16 *__restrict__ dl, float *__restrict__ part,
+// A step is 32 tokens, 8 kg .. 8 kg + 7 in a lane, in bf16 (one instruction), and 16, kg + 4 j, in fp32 (four).
+template <typename T, int ME>
+__device__ __forceinline__ void dw_block(const T *__restrict__ u, const T *__restrict__ dl, float *__restrict__ part,
                                          float (*lds)[LB_COLS + 4], int64_t tokens, int D, int E, int col, int eb, int64_t split,
                                          int64_t share)
 {
+    constexpr bool BF = sizeof(T) == 2;
+    constexpr int STEP = dw_step<T>(), R = STEP / 4, EVERY = BF ? 1 : 4;        // rows of a lane, and the distance between them
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
+    const int own = BF ? 8 * kg : kg;                                           // the lane's first row of a step
     const int64_t t0 = split * share, t1 = min(t0 + share, tokens);
     const Cols c(col * LB_COLS + 8 * n, D, 8), x(eb * 16 * ME + ME * n, E, ME);
     f32x4_t acc[ME][8] = {};
     struct Step {
-        Piece<bf16, 8> u[8];
-        uint32_t g[8][(ME + 1) / 2];
+        Piece<T, 8> u[R];
+        uint32_t g[R][BF ? (ME + 1) / 2 : ME];
     };
-    const uint32_t uo = 8 * kg * D + c.at, go = 8 * kg * E + x.at;
-    auto experts = [&](uint32_t *g, const bf16 *p) __attribute__((always_inline)) {
-        if constexpr (ME == 1) g[0] = p->bits;
-        else if constexpr (ME == 2) g[0] = *reinterpret_cast<const any_u32_t *>(p);
-        else {
+    const uint32_t uo = own * D + c.at, go = own * E + x.at;
+    auto experts = [&](uint32_t *g, const T *p) __attribute__((always_inline)) {
+        constexpr int BYTES = ME * sizeof(T);
+        if constexpr (BYTES == 2) g[0] = *reinterpret_cast<const uint16_t *>(p);
+        else if constexpr (BYTES == 4) g[0] = *reinterpret_cast<const any_u32_t *>(p);
+        else if constexpr (BYTES == 8) {
             const any_u32x2_t v = *reinterpret_cast<const any_u32x2_t *>(p);
             g[0] = v.x; g[1] = v.y;
+        } else {
+            const any_u32x4_t v = *reinterpret_cast<const any_u32x4_t *>(p);
+            g[0] = v.x; g[1] = v.y; g[2] = v.z; g[3] = v.w;
         }
     };
     auto fetch = [&](Step &s, int64_t t) __attribute__((always_inline)) {
-        const bf16 *ur = u + t * D, *gr = dl + t * E;
-        if (t + 32 <= t1 && D >= 8) {
+        const T *ur = u + t * D, *gr = dl + t * E;
+        if (t + STEP <= t1 && D >= 8) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j, ur += D, gr += E) {
+            for (int j = 0; j < R; ++j, ur += EVERY * D, gr += EVERY * E) {
                 s.u[j].template load<false>(ur + uo, 8);
                 experts(s.g[j], gr + go);
             }
@@ -66,32 +80,41 @@ __device__ __forceinline__ void dw_block(const bf16 *__restrict__ u, const bf16 
         }
         // tokens that are not the block's add nothing, whatever memory holds there
 #pragma unroll
-        for (int j = 0; j < 8; ++j, ur += D, gr += E) {
-            const bool in = t + 8 * kg + j < t1;
+        for (int j = 0; j < R; ++j, ur += EVERY * D, gr += EVERY * E) {
+            const bool in = t + own + EVERY * j < t1;
             s.u[j].template load<true>(ur + uo, in ? (D >= 8 ? 8 : D - c.at) : 0);
 #pragma unroll
-            for (int i = 0; i < (ME + 1) / 2; ++i) s.g[j][i] = 0;
+            for (uint32_t &g : s.g[j]) g = 0;
             if (in) experts(s.g[j], gr + go);
         }
     };
     Step next;
-    int64_t t = t0 + 32 * wave;
+    int64_t t = t0 + STEP * wave;
     if (t < t1) fetch(next, t);
-    for (; t < t1; t += 32 * LB_WAVES) {
+    for (; t < t1; t += STEP * LB_WAVES) {
         const Step s = next;
-        if (t + 32 * LB_WAVES < t1) fetch(next, t + 32 * LB_WAVES);
-        uint32_t a[ME][4];
+        if (t + STEP * LB_WAVES < t1) fetch(next, t + STEP * LB_WAVES);
+        if constexpr (BF) {
+            uint32_t a[ME][4];
 #pragma unroll
-        for (int j = 0; j < ME; ++j)
+            for (int j = 0; j < ME; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) a[j][q] = pair_of(s.g[2 * q][j / 2], s.g[2 * q + 1][j / 2], j);
+                for (int q = 0; q < 4; ++q) a[j][q] = pair_of(s.g[2 * q][j / 2], s.g[2 * q + 1][j / 2], j);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint32_t b[4];
+            for (int i = 0; i < 8; ++i) {
+                uint32_t b[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) b[q] = pair_of(s.u[2 * q].v[i / 2], s.u[2 * q + 1].v[i / 2], i);
+                for (int q = 0; q < 4; ++q) b[q] = pair_of(s.u[2 * q].v[i / 2], s.u[2 * q + 1].v[i / 2], i);
 #pragma unroll
-            for (int j = 0; j < ME; ++j) acc[j][i] = mfma16(a[j], b, acc[j][i]);
+                for (int j = 0; j < ME; ++j) acc[j][i] = mfma16(a[j], b, acc[j][i]);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int j = 0; j < ME; ++j) acc[j][i] = mfma4(s.g[r][j], s.u[r].v[i], acc[j][i]);
         }
     }
     // lds[e][column], counted from the block's first
@@ -117,26 +140,29 @@ __device__ __forceinline__ void dw_block(const bf16 *__restrict__ u, const bf16 
     }
 }
 
-// du: KS steps of 32 experts, NT tiles of 16 columns (16 NT columns to a wave, NT consecutive ones to a lane)
-template <int KS, int NT>
-__device__ __forceinline__ void du_block(const bf16 *__restrict__ Wg, const bf16 *__restrict__ dl, const bf16 *du_add, bf16 *du,
+// du: KS steps of 32 (bf16) or 16 (fp32) experts, NT tiles of 16 columns (16 NT columns to a wave, NT consecutive ones to a
+// lane).  In a step a lane has the experts 8 kg .. 8 kg + 7, one instruction, or 4 kg .. 4 kg + 3, one instruction for each.
+template <typename T, int KS, int NT>
+__device__ __forceinline__ void du_block(const T *__restrict__ Wg, const T *__restrict__ dl, const T *du_add, T *du,
                                          int64_t tokens, int D, int E, int col, int64_t split, int64_t share)
 {
+    constexpr bool BF = sizeof(T) == 2, AHEAD = KS * (BF ? 2 : 1) <= 4;         // the operand of many experts leaves no registers
+    constexpr int R = BF ? 8 : 4;                                               // experts of a lane in a step
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
     const int64_t t0 = split * share, t1 = min(t0 + share, tokens);
     const Cols c(col * 16 * NT + NT * n, D, NT);
     const int width = D >= NT ? (c.own < D ? NT : 0) : D - c.at;       // elements of the lane's piece that exist
     struct Step {
-        Piece<bf16, 8> a[KS];
-        Piece<bf16, NT> add[4];
+        Piece<T, R> a[KS];
+        Piece<T, NT> add[4];
     };
     auto fetch = [&](Step &s, int64_t t) __attribute__((always_inline)) {
-        const bf16 *g = dl + t * E, *add = du_add + t * D;
+        const T *g = dl + t * E, *add = du_add + t * D;
         const int left = (int)min((int64_t)16, t1 - t);
         const uint32_t row = min(n, left - 1) * E;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            const int e = 32 * k + 8 * kg;
+            const int e = 4 * R * k + R * kg;
             s.a[k].template load<true>(g + row + e, E - e);
         }
         if (du_add) {
@@ -147,42 +173,55 @@ __device__ __forceinline__ void du_block(const bf16 *__restrict__ Wg, const bf16
     };
     Step next;
     int64_t t = t0 + 16 * wave;
-    if (t < t1) fetch(next, t);
+    if (AHEAD && t < t1) fetch(next, t);
     uint32_t w[KS][NT][4];
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-        Piece<bf16, NT> p[8];
+        Piece<T, NT> p[R];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int e = 32 * k + 8 * kg + j;
+        for (int j = 0; j < R; ++j) {
+            const int e = 4 * R * k + R * kg + j;
             p[j].template load<true>(Wg + (uint32_t)(e * D + c.at), e < E ? width : 0);
         }
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) w[k][i][q] = pair_of(p[2 * q].v[i / 2], p[2 * q + 1].v[i / 2], i);
+            for (int q = 0; q < 4; ++q) {
+                if constexpr (BF) w[k][i][q] = pair_of(p[2 * q].v[i / 2], p[2 * q + 1].v[i / 2], i);
+                else w[k][i][q] = p[q].v[i];
+            }
     }
     for (; t < t1; t += 16 * LB_WAVES) {
-        const Step s = next;
-        if (t + 16 * LB_WAVES < t1) fetch(next, t + 16 * LB_WAVES);
+        Step s;
+        if constexpr (AHEAD) {
+            s = next;
+            if (t + 16 * LB_WAVES < t1) fetch(next, t + 16 * LB_WAVES);
+        } else
+            fetch(s, t);
         f32x4_t acc[NT] = {};
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int i = 0; i < NT; ++i) acc[i] = mfma16(s.a[k].v, w[k][i], acc[i]);
-        bf16 *const out = du + t * D;
+            for (int i = 0; i < NT; ++i) {
+                if constexpr (BF) acc[i] = mfma16(s.a[k].v, w[k][i], acc[i]);
+                else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[i] = mfma4(s.a[k].v[q], w[k][i][q], acc[i]);
+                }
+            }
+        T *const out = du + t * D;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             float o[NT];
 #pragma unroll
             for (int i = 0; i < NT; ++i) o[i] = acc[i][v] + (du_add ? s.add[v].get(i) : 0.f);
             if (t + 4 * kg + v >= t1) continue;
-            bf16 *const p = out + (uint32_t)((4 * kg + v) * D + c.at);
+            T *const p = out + (uint32_t)((4 * kg + v) * D + c.at);
             if (c.at == c.own) store_piece<true>(p, o, width);
             else {
 #pragma unroll
                 for (int i = 0; i < NT; ++i)
-                    if (i >= c.own - c.at) p[i] = from_float<bf16>(o[i]);
+                    if (i >= c.own - c.at) p[i] = from_float<T>(o[i]);
             }
         }
     }
@@ -192,21 +231,21 @@ __device__ __forceinline__ void du_block(const bf16 *__restrict__ Wg, const bf16
 struct Shares { int64_t share, count; };
 
 // One launch does both: the first wblocks blocks sum dW, the others write du, so that the two streams of memory overlap.
-template <int ME, int KS, int NT>
-__global__ void __launch_bounds__(64 * LB_WAVES) __attribute__((amdgpu_waves_per_eu(KS == 8 ? 1 : ME == 4 ? 2 : 3)))
-linear_bwd_bf16_kernel(const bf16 *__restrict__ u, const bf16 *__restrict__ Wg, const bf16 *__restrict__ dl, const bf16 *du_add,
-                       bf16 *du, float *__restrict__ part, int64_t tokens, int D, int E, unsigned wblocks, Shares ws, Shares us)
+template <typename T, int ME, int KS, int NT>
+__global__ void __launch_bounds__(64 * LB_WAVES) __attribute__((amdgpu_waves_per_eu(ME == 4 || sizeof(T) == 4 ? 2 : 3)))
+linear_bwd_kernel(const T *__restrict__ u, const T *__restrict__ Wg, const T *__restrict__ dl, const T *du_add, T *du,
+                  float *__restrict__ part, int64_t tokens, int D, int E, unsigned wblocks, Shares ws, Shares us)
 {
     __shared__ float lds[16 * ME][LB_COLS + 4];
     if (blockIdx.x < wblocks) {
         // the blocks of one share and its columns, which read the same u, follow each other on one XCD
         const int cols = (D + LB_COLS - 1) / LB_COLS, eblocks = (E + 16 * ME - 1) / (16 * ME);
         const int64_t id = xcd_logical_id(blockIdx.x, wblocks), col = id / eblocks % cols, split = id / eblocks / cols;
-        if (split < ws.count) dw_block<ME>(u, dl, part, lds, tokens, D, E, (int)col, (int)(id % eblocks), split, ws.share);
+        if (split < ws.count) dw_block<T, ME>(u, dl, part, lds, tokens, D, E, (int)col, (int)(id % eblocks), split, ws.share);
     } else {
         const int cols = (D + 16 * NT - 1) / (16 * NT);
         const int64_t id = blockIdx.x - wblocks;
-        du_block<KS, NT>(Wg, dl, du_add, du, tokens, D, E, (int)(id % cols), id / cols, us.share);
+        du_block<T, KS, NT>(Wg, dl, du_add, du, tokens, D, E, (int)(id % cols), id / cols, us.share);
     }
 }
 
@@ -214,31 +253,6 @@ __global__ void __launch_bounds__(512)
 linear_reduce_kernel(const float *__restrict__ part, int rows, int64_t n, float *__restrict__ dW)
 {
     sum_rows(part, rows, n, [&](int64_t c, float s) { dW[c] = s; });
-}
-
-// fp32: one element by one, for now
-__global__ void __launch_bounds__(256)
-linear_du_f32_kernel(const float *__restrict__ Wg, const float *__restrict__ dl, const float *du_add, float *du, int64_t tokens, int D, int E)
-{
-    const int64_t n = tokens * D;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t t = i / D, d = i % D;
-        float s = 0.f;
-        for (int e = 0; e < E; ++e) s += dl[t * E + e] * Wg[e * (int64_t)D + d];
-        if (du_add) s += du_add[i];
-        du[i] = s;
-    }
-}
-__global__ void __launch_bounds__(256)
-linear_dw_f32_kernel(const float *__restrict__ u, const float *__restrict__ dl, float *__restrict__ part, int64_t tokens, int D, int E,
-                     int64_t share)
-{
-    const int d = blockIdx.x * 256 + threadIdx.x, e = blockIdx.y;
-    if (d >= D) return;
-    const int64_t t0 = blockIdx.z * share, t1 = min(t0 + share, tokens);
-    float s = 0.f;
-    for (int64_t t = t0; t < t1; ++t) s += dl[t * E + e] * u[t * D + d];
-    part[((int64_t)blockIdx.z * E + e) * D + d] = s;
 }
 
 namespace {
@@ -254,7 +268,45 @@ int experts_of(int E) { return E <= 16 ? 16 : E <= 32 ? 32 : 64; }              
 // Blocks that the chip holds at once at the kernels' registers, half of them for each product.
 int64_t blocks_of(int E) { return E <= 32 ? 512 : 256; }
 int64_t dw_per_share(int D, int E) { return (int64_t)((D + LB_COLS - 1) / LB_COLS) * ((E + experts_of(E) - 1) / experts_of(E)); }
-Shares dw_shares(int64_t tokens, int D, int E) { return shares_of(tokens, dw_per_share(D, E), 32 * LB_WAVES, blocks_of(E)); }
+// (in steps of bf16 tokens, of which those of fp32 are half: the shares do not depend on the type)
+Shares dw_shares(int64_t tokens, int D, int E) { return shares_of(tokens, dw_per_share(D, E), dw_step<bf16>() * LB_WAVES, blocks_of(E)); }
+
+template <typename T>
+swimba_status linear_bwd(int64_t tokens, int D, int E, const void *u, const void *Wg, const void *dl, const void *du_add, void *du,
+                         bool dW, float *part, hipStream_t st)
+{
+    const Shares sh = dw_shares(tokens, D, E);
+    auto go = [&](auto me, auto ks, auto nt) {
+        const int64_t cols = (D + 16 * nt - 1) / (16 * nt);
+        const Shares us = shares_of(tokens, cols, 16 * LB_WAVES, blocks_of(E));
+        const unsigned wb = dW ? (unsigned)xcd_padded(dw_per_share(D, E) * sh.count) : 0;
+        const unsigned ub = du ? (unsigned)(cols * us.count) : 0;
+        if (wb + ub == 0) return;
+        hipLaunchKernelGGL((linear_bwd_kernel<T, me(), ks(), nt()>), dim3(wb + ub), dim3(64 * LB_WAVES), 0, st, (const T *)u,
+                           (const T *)Wg, (const T *)dl, (const T *)du_add, (T *)du, part, tokens, D, E, wb, sh, us);
+    };
+    constexpr std::integral_constant<int, 1> one;
+    constexpr std::integral_constant<int, 2> two;
+    constexpr std::integral_constant<int, 4> four;
+    constexpr std::integral_constant<int, 8> eight;
+    constexpr std::integral_constant<int, 16> sixteen;
+    // W's operand is at most 128 registers: with more than 128 (bf16) or 32 (fp32) experts, of fewer columns
+    if constexpr (sizeof(T) == 2) {
+        if (E <= 16) go(one, one, eight);
+        else if (E <= 32) go(two, one, eight);
+        else if (E <= 64) go(four, two, eight);
+        else if (E <= 128) go(four, four, eight);
+        else go(four, eight, four);
+    } else {
+        if (E <= 16) go(one, one, eight);
+        else if (E <= 32) go(two, two, eight);
+        else if (E <= 64) go(four, four, four);
+        else if (E <= 128) go(four, eight, four);
+        else go(four, sixteen, two);
+    }
+    SWIMBA_CHECK_LAUNCH();
+    return SWIMBA_OK;
+}
 
 }  // namespace
 
@@ -263,37 +315,17 @@ size_t router_linear_bwd_bytes(int64_t tokens, int D, int E) { return (size_t)dw
 swimba_status launch_router_linear_bwd(int64_t tokens, int D, int E, int io_dtype, const void *u, const void *Wg, const void *dl,
                                        const void *du_add, void *du, float *dW, void *work, hipStream_t st)
 {
-    const Shares sh = dw_shares(tokens, D, E);
-    float *part = (float *)work;
-    if (tokens > 0 && io_dtype == SWIMBA_BF16) {
-        auto go = [&](auto kernel, int wide) {
-            const int64_t cols = (D + wide - 1) / wide;
-            const Shares us = shares_of(tokens, cols, 16 * LB_WAVES, blocks_of(E));
-            const unsigned wb = dW ? (unsigned)xcd_padded(dw_per_share(D, E) * sh.count) : 0;
-            const unsigned ub = du ? (unsigned)(cols * us.count) : 0;
-            if (wb + ub == 0) return;
-            hipLaunchKernelGGL(kernel, dim3(wb + ub), dim3(64 * LB_WAVES), 0, st, (const bf16 *)u, (const bf16 *)Wg, (const bf16 *)dl,
-                               (const bf16 *)du_add, (bf16 *)du, part, tokens, D, E, wb, sh, us);
-        };
-        if (E <= 16) go(linear_bwd_bf16_kernel<1, 1, 8>, 128);
-        else if (E <= 32) go(linear_bwd_bf16_kernel<2, 1, 8>, 128);
-        else if (E <= 64) go(linear_bwd_bf16_kernel<4, 2, 8>, 128);
-        else if (E <= 128) go(linear_bwd_bf16_kernel<4, 4, 8>, 128);
-        else go(linear_bwd_bf16_kernel<4, 8, 4>, 64);
-        SWIMBA_CHECK_LAUNCH();
-    } else if (tokens > 0) {
-        if (du)
-            hipLaunchKernelGGL(linear_du_f32_kernel, dim3((unsigned)((tokens * D + 255) / 256 < 65536 ? (tokens * D + 255) / 256 : 65536)),
-                               dim3(256), 0, st, (const float *)Wg, (const float *)dl, (const float *)du_add, (float *)du, tokens, D, E);
-        SWIMBA_CHECK_LAUNCH();
-        if (dW)
-            hipLaunchKernelGGL(linear_dw_f32_kernel, dim3((unsigned)((D + 255) / 256), (unsigned)E, (unsigned)sh.count), dim3(256), 0, st,
-                               (const float *)u, (const float *)dl, part, tokens, D, E, sh.share);
-        SWIMBA_CHECK_LAUNCH();
+    const int64_t shares = dw_shares(tokens, D, E).count;
+    // the sums of one share are dW itself
+    float *const part = shares == 1 ? dW : (float *)work;
+    if (tokens > 0) {
+        const auto go = io_dtype == SWIMBA_BF16 ? linear_bwd<bf16> : linear_bwd<float>;
+        const swimba_status s = go(tokens, D, E, u, Wg, dl, du_add, du, dW != nullptr, part, st);
+        if (s != SWIMBA_OK) return s;
     }
-    if (dW) {
+    if (dW && shares != 1) {
         const int64_t n = (int64_t)E * D;
-        hipLaunchKernelGGL(linear_reduce_kernel, dim3((unsigned)((n + 31) / 32)), dim3(512), 0, st, part, (int)sh.count, n, dW);
+        hipLaunchKernelGGL(linear_reduce_kernel, dim3((unsigned)((n + 31) / 32)), dim3(512), 0, st, part, (int)shares, n, dW);
         SWIMBA_CHECK_LAUNCH();
     }
     return SWIMBA_OK;

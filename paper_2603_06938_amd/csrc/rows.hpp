@@ -15,7 +15,7 @@ typedef uint32_t __attribute__((ext_vector_type(4), aligned(2))) any_u32x4_t;
 typedef uint32_t __attribute__((ext_vector_type(2), aligned(2))) any_u32x2_t;
 typedef uint32_t __attribute__((aligned(2))) any_u32_t;
 
-// W (4 or 8) consecutive elements of a row as they lie in memory: loaded long before they are used, they take few registers.
+// W (2, 4 or 8) consecutive elements of a row as they lie in memory: loaded long before they are used, they take few registers.
 template <typename T, int W> struct Piece {
     static constexpr int WORDS = W * (int)sizeof(T) / 4;
     uint32_t v[WORDS];
@@ -23,7 +23,9 @@ template <typename T, int W> struct Piece {
     template <bool TAIL> __device__ __forceinline__ void load(const T *p, int n)
     {
         if (n >= W) {
-            if constexpr (WORDS == 2) {
+            if constexpr (WORDS == 1) {
+                v[0] = *reinterpret_cast<const any_u32_t *>(p);
+            } else if constexpr (WORDS == 2) {
                 const any_u32x2_t a = *reinterpret_cast<const any_u32x2_t *>(p);
                 v[0] = a.x; v[1] = a.y;
             } else {
@@ -63,7 +65,8 @@ template <bool TAIL, typename T, int W> __device__ __forceinline__ void store_pi
             if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(f[i]);
             else v[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
         }
-        if constexpr (Piece<T, W>::WORDS == 2) *reinterpret_cast<any_u32x2_t *>(p) = any_u32x2_t{v[0], v[1]};
+        if constexpr (Piece<T, W>::WORDS == 1) *reinterpret_cast<any_u32_t *>(p) = v[0];
+        else if constexpr (Piece<T, W>::WORDS == 2) *reinterpret_cast<any_u32x2_t *>(p) = any_u32x2_t{v[0], v[1]};
         else {
 #pragma unroll
             for (int i = 0; i < Piece<T, W>::WORDS; i += 4)
