@@ -7,14 +7,18 @@
 
 namespace swimba {
 
-// A row lies in the registers of WPR waves, W NV elements to a lane: piece i of lane l are the elements from W (l + 64 WPR i) on.
-// sums of N values over the row's waves, in every lane; `round` alternates, so that one barrier a round is enough
-template <int WPR, int N>
+// A row lies in the registers of LPR lanes (16 to 64 of a wave, or all of 4, 8 or 16 waves), W NV elements to a lane: piece i of
+// lane l are the elements from W (l + LPR i) on.
+constexpr int norm_threads(int LPR) { return LPR < 256 ? 256 : LPR; }
+constexpr int rows_per_block(int LPR) { return norm_threads(LPR) / LPR; }
+
+// sums of N values over the row's lanes, in every one of them; `round` alternates, so that one barrier a round is enough
+template <int LPR, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[N][16], int round)
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
-    if constexpr (WPR > 1) {
+    for (int i = 0; i < N; ++i) v[i] = group_sum<LPR < 64 ? LPR : 64>(v[i]);
+    if constexpr (LPR > 64) {
         const int wave = threadIdx.x >> 6;
 #pragma unroll
         for (int i = 0; i < N; ++i) lds[round & 1][i][wave] = v[i];
@@ -23,25 +27,28 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[N][16], int
         for (int i = 0; i < N; ++i) {
             v[i] = 0.f;
 #pragma unroll
-            for (int w = 0; w < WPR; ++w) v[i] += lds[round & 1][i][w];
+            for (int w = 0; w < LPR / 64; ++w) v[i] += lds[round & 1][i][w];
         }
     }
 }
 
-constexpr int norm_threads(int WPR) { return WPR < 4 ? 256 : 64 * WPR; }
-constexpr int rows_per_block(int WPR) { return norm_threads(WPR) / 64 / WPR; }
+// first row of the thread's lanes in the block
+template <int LPR> __device__ __forceinline__ int row_slot()
+{
+    return LPR < 64 ? threadIdx.x / LPR : __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / (LPR / 64);
+}
 
-template <typename T, typename R, int W, int NV, int WPR, bool TAIL>
-__global__ void __launch_bounds__(norm_threads(WPR))
+template <typename T, typename R, int W, int NV, int LPR, bool TAIL>
+__global__ void __launch_bounds__(norm_threads(LPR))
 norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
                 T *__restrict__ u, R *sum, float *__restrict__ mean, float *__restrict__ rstd, int64_t tokens, int D)
 {
     __shared__ float lds[2][1][16];
-    constexpr int RPB = rows_per_block(WPR);                   // rows a block has at a time
-    const int lane = threadIdx.x % (64 * WPR), slot = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / WPR;
+    constexpr int RPB = rows_per_block(LPR);                   // rows a block has at a time
+    const int lane = threadIdx.x % LPR;
     const float width = (float)D;
     int round = 0;
-    for (int64_t t = (int64_t)blockIdx.x * RPB + slot; t < tokens; t += (int64_t)gridDim.x * RPB) {
+    for (int64_t t = (int64_t)blockIdx.x * RPB + row_slot<LPR>(); t < tokens; t += (int64_t)gridDim.x * RPB) {
         const T *const xr = x + t * D;
         const R *const rr = residual + t * D;
         R *const sr = sum + t * D;
@@ -50,14 +57,14 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
         Piece<R, W> pr[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t d = W * (lane + 64 * WPR * i);
+            const uint32_t d = W * (lane + LPR * i);
             px[i].template load<TAIL>(xr + d, D - (int)d);
             if (residual) pr[i].template load<TAIL>(rr + d, D - (int)d);
         }
         float r[NV][W], s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t d = W * (lane + 64 * WPR * i);
+            const uint32_t d = W * (lane + LPR * i);
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 r[i][j] = px[i].get(j);
@@ -66,19 +73,19 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
             }
             if (sum) store_piece<TAIL>(sr + d, r[i], D - (int)d);
         }
-        row_sums<WPR>(s, lds, round++);
+        row_sums<LPR>(s, lds, round++);
         const float m = s[0] / width;                          // divided, not multiplied: a constant row is centred to zero
         s[0] = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int n = D - W * (lane + 64 * WPR * i);
+            const int n = D - W * (lane + LPR * i);
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 r[i][j] -= m;
                 s[0] += j < n ? r[i][j] * r[i][j] : 0.f;
             }
         }
-        row_sums<WPR>(s, lds, round++);
+        row_sums<LPR>(s, lds, round++);
         const float is = 1.0f / sqrtf(s[0] / width + eps);
         if (lane == 0) {
             if (mean) mean[t] = m;
@@ -86,7 +93,7 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t d = W * (lane + 64 * WPR * i);
+            const uint32_t d = W * (lane + LPR * i);
             Piece<float, W> g, b;
             if (gamma) g.template load<TAIL>(gamma + d, D - (int)d);
             if (beta) b.template load<TAIL>(beta + d, D - (int)d);
@@ -97,20 +104,20 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
     }
 }
 
-// The rows are walked by as many blocks as keep sums of their own; the next row's pieces are under way while a row is summed.
-template <typename T, typename R, int W, int NV, int WPR, bool TAIL>
-__global__ void __launch_bounds__(norm_threads(WPR))
+// The blocks keep sums of their own for dgamma and dbeta: part (blocks, 2, D), or the two themselves where there is one block.
+template <typename T, typename R, int W, int NV, int LPR, bool TAIL>
+__global__ void __launch_bounds__(norm_threads(LPR))
 norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *__restrict__ gamma,
                 const float *__restrict__ mean, const float *__restrict__ rstd, const R *d_sum, R *dx, T *__restrict__ dx_io,
-                float *__restrict__ part, int64_t tokens, int D)
+                float *__restrict__ pgamma, float *__restrict__ pbeta, int64_t tokens, int D)
 {
-    constexpr int RPB = rows_per_block(WPR), SPAN = 64 * WPR * W;
+    constexpr int RPB = rows_per_block(LPR), SPAN = LPR * W;
+    constexpr bool AHEAD = LPR < 1024;                         // 1024 threads have no registers for it, nor for the gain
     __shared__ float lds[2][2][16];
     __shared__ float comb[RPB > 1 ? RPB * 2 * NV * SPAN : 1];
-    const int lane = threadIdx.x % (64 * WPR), slot = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / WPR;
+    const int lane = threadIdx.x % LPR, slot = row_slot<LPR>();
     const float width = (float)D;
     const int64_t stride = (int64_t)gridDim.x * RPB;
-    constexpr bool AHEAD = WPR < 16;                           // 1024 threads have no registers for it, nor for the gain
     float dg[NV][W] = {}, db[NV][W] = {}, w[NV][W];
     auto gain = [&] {
 #pragma unroll
@@ -168,7 +175,7 @@ norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *
                 s[1] += g[i][j] * xh[i][j];
             }
         }
-        row_sums<WPR>(s, lds, round);
+        row_sums<LPR>(s, lds, round);
         const float mg = s[0] / width, mx = s[1] / width;
         R *const out = dx + t * D;
         T *const out_io = dx_io + t * D;
@@ -183,8 +190,8 @@ norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *
             if (dx_io) store_piece<TAIL>(out_io + d, g[i], D - (int)d);
         }
     }
-    if (!part) return;
-    float *p = part + (int64_t)blockIdx.x * 2 * D;              // (blocks, 2, D)
+    float *const pg = pgamma + (int64_t)blockIdx.x * 2 * D, *const pb = pbeta + (int64_t)blockIdx.x * 2 * D;
+    if (!pgamma && !pbeta) return;
     if constexpr (RPB > 1) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -195,19 +202,20 @@ norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *
                 comb[(slot * 2 + 1) * NV * SPAN + d] = db[i][j];
             }
         __syncthreads();
-        for (int c = threadIdx.x; c < 2 * D; c += norm_threads(WPR)) {
+        for (int c = threadIdx.x; c < 2 * D; c += norm_threads(LPR)) {
             const int at = c < D ? c : c - D + NV * SPAN;
             float s = 0.f;
 #pragma unroll
             for (int k = 0; k < RPB; ++k) s += comb[k * 2 * NV * SPAN + at];
-            p[c] = s;
+            if (c < D && pgamma) pg[c] = s;
+            if (c >= D && pbeta) pb[c - D] = s;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int d = W * lane + SPAN * i;
-            store_piece<TAIL>(p + d, dg[i], D - d);
-            store_piece<TAIL>(p + D + d, db[i], D - d);
+            const uint32_t d = W * lane + SPAN * i;
+            if (pgamma) store_piece<TAIL>(pg + d, dg[i], D - (int)d);
+            if (pbeta) store_piece<TAIL>(pb + d, db[i], D - (int)d);
         }
     }
 }
@@ -224,70 +232,91 @@ norm_reduce_kernel(const float *__restrict__ part, int rows, int D, float *__res
 
 namespace {
 
-// Waves of a row, so that a lane has 16 elements at most: one up to 1024 features, then four, eight and sixteen.
-int waves_per_row(int D) { return D <= 1024 ? 1 : D <= 4096 ? 4 : D <= 8192 ? 8 : 16; }
+// Lanes of a row: one piece to a lane up to 256 features, 16 elements at most beyond.
+int lanes_per_row(int D) { return D <= 64 ? 16 : D <= 128 ? 32 : D <= 1024 ? 64 : D <= 4096 ? 256 : D <= 8192 ? 512 : 1024; }
 
-// f(number of pieces, waves of a row, whether the last piece may be short) as constants
-template <int W, typename F>
+// f(elements of a piece, pieces, lanes of a row, whether the last piece may be short) as constants.  Pieces of 16 bytes for
+// wide rows of bf16 alone (32768 x 2048 forward 62 us with 8 bytes, 58.6 with 16; backward 85 and 79); of 4 elements elsewhere,
+// which fill the lanes of a narrow row better.
+template <typename T, typename R, typename F>
 void with_row(int D, F &&f)
 {
     using std::integral_constant;
-    const int wpr = waves_per_row(D), nv = (D + 64 * wpr * W - 1) / (64 * wpr * W);
-    auto tail = [&](auto n, auto waves) {
-        if (D % W) f(n, waves, std::true_type());
-        else f(n, waves, std::false_type());
-    };
-    constexpr integral_constant<int, 16 / W> most;
-    constexpr integral_constant<int, 8 / W> some;
-    if (wpr == 16) return tail(most, integral_constant<int, 16>());
-    if (wpr == 8) return tail(most, integral_constant<int, 8>());
-    if (wpr == 4) return nv > some ? tail(most, integral_constant<int, 4>()) : tail(some, integral_constant<int, 4>());
     constexpr integral_constant<int, 1> one;
-    if (nv > 12 / W) return tail(most, one);
-    if (nv > 8 / W) return tail(integral_constant<int, (12 + W - 1) / W>(), one);
-    return nv > 4 / W ? tail(some, one) : tail(integral_constant<int, (4 + W - 1) / W>(), one);
+    constexpr integral_constant<int, 2> two;
+    constexpr integral_constant<int, 3> three;
+    constexpr integral_constant<int, 4> four;
+    constexpr integral_constant<int, sizeof(T) + sizeof(R) == 4 ? 8 : 4> wide;
+    constexpr integral_constant<int, 16 / wide> most;
+    auto tail = [&](auto w, auto pieces, auto lanes) {
+        if (D % w) f(w, pieces, lanes, std::true_type());
+        else f(w, pieces, lanes, std::false_type());
+    };
+    switch (lanes_per_row(D)) {
+    case 16: return tail(four, one, integral_constant<int, 16>());
+    case 32: return tail(four, one, integral_constant<int, 32>());
+    case 64: {
+        constexpr integral_constant<int, 64> lanes;
+        return D <= 256 ? tail(four, one, lanes) : D <= 512 ? tail(four, two, lanes) : D <= 768 ? tail(four, three, lanes) : tail(four, four, lanes);
+    }
+    case 256: {
+        constexpr integral_constant<int, 256> lanes;
+        return D <= 2048 ? tail(wide, integral_constant<int, most / 2>(), lanes) : tail(wide, most, lanes);
+    }
+    case 512: return tail(wide, most, integral_constant<int, 512>());
+    default: return tail(wide, most, integral_constant<int, 1024>());
+    }
 }
 
-constexpr int NORM_W = 4;                  // elements of a piece
+int64_t blocks_for(int64_t tokens, int rpb, int64_t most)
+{
+    const int64_t need = (tokens + rpb - 1) / rpb;
+    return need < most ? need : most;
+}
 
 template <typename T, typename R>
 swimba_status norm_fwd(int64_t tokens, int D, const void *x, const void *residual, const float *gamma, const float *beta,
                        float eps, void *u, void *sum, float *mean, float *rstd, hipStream_t st)
 {
-    with_row<NORM_W>(D, [&](auto nv, auto wpr, auto tail) {
-        const int64_t need = (tokens + rows_per_block(wpr) - 1) / rows_per_block(wpr);
-        hipLaunchKernelGGL((norm_fwd_kernel<T, R, NORM_W, nv(), wpr(), tail()>), dim3((unsigned)(need < (1 << 20) ? need : (1 << 20))),
-                           dim3(norm_threads(wpr)), 0, st, (const T *)x, (const R *)residual, gamma, beta, eps, (T *)u, (R *)sum, mean,
+    auto go = [&](auto w, auto nv, auto lpr, auto tail) {
+        hipLaunchKernelGGL((norm_fwd_kernel<T, R, w(), nv(), lpr(), tail()>), dim3((unsigned)blocks_for(tokens, rows_per_block(lpr), 1 << 20)),
+                           dim3(norm_threads(lpr)), 0, st, (const T *)x, (const R *)residual, gamma, beta, eps, (T *)u, (R *)sum, mean,
                            rstd, tokens, D);
-    });
+    };
+    with_row<T, R>(D, go);
     SWIMBA_CHECK_LAUNCH();
     return SWIMBA_OK;
 }
 
-// most blocks of the backward pass, which keep sums of their own
+// Blocks of the backward pass, which keep sums of their own: one, whose sums need no second launch, for up to four rounds of
+// its rows.
 int64_t bwd_blocks(int64_t tokens, int D)
 {
-    const int rpb = rows_per_block(waves_per_row(D));
-    const int64_t need = (tokens + rpb - 1) / rpb, most = waves_per_row(D) == 16 ? 256 : 512;
-    return need < most ? need : most;
+    const int rpb = rows_per_block(lanes_per_row(D));
+    return tokens <= 4 * rpb ? (tokens > 0) : blocks_for(tokens, rpb, lanes_per_row(D) == 1024 ? 256 : 512);
 }
 
 template <typename T, typename R>
 swimba_status norm_bwd(int64_t tokens, int D, const void *du, const void *r, const float *gamma, const float *mean,
-                       const float *rstd, const void *d_sum, void *dx, void *dx_io, float *part, hipStream_t st)
+                       const float *rstd, const void *d_sum, void *dx, void *dx_io, float *pgamma, float *pbeta, hipStream_t st)
 {
-    with_row<NORM_W>(D, [&](auto nv, auto wpr, auto tail) {
-        hipLaunchKernelGGL((norm_bwd_kernel<T, R, NORM_W, nv(), wpr(), tail()>), dim3((unsigned)bwd_blocks(tokens, D)),
-                           dim3(norm_threads(wpr)), 0, st, (const T *)du, (const R *)r, gamma, mean, rstd, (const R *)d_sum, (R *)dx,
-                           (T *)dx_io, part, tokens, D);
-    });
+    auto go = [&](auto w, auto nv, auto lpr, auto tail) {
+        hipLaunchKernelGGL((norm_bwd_kernel<T, R, w(), nv(), lpr(), tail()>), dim3((unsigned)bwd_blocks(tokens, D)),
+                           dim3(norm_threads(lpr)), 0, st, (const T *)du, (const R *)r, gamma, mean, rstd, (const R *)d_sum, (R *)dx,
+                           (T *)dx_io, pgamma, pbeta, tokens, D);
+    };
+    with_row<T, R>(D, go);
     SWIMBA_CHECK_LAUNCH();
     return SWIMBA_OK;
 }
 
 }  // namespace
 
-size_t layer_norm_bwd_bytes(int64_t tokens, int D) { return (size_t)bwd_blocks(tokens, D) * 2 * D * sizeof(float); }
+size_t layer_norm_bwd_bytes(int64_t tokens, int D)
+{
+    const int64_t n = bwd_blocks(tokens, D);
+    return n > 1 ? (size_t)n * 2 * D * sizeof(float) : 0;
+}
 
 swimba_status launch_layer_norm(int64_t tokens, int D, int io_dtype, int res_dtype, const void *x, const void *residual,
                                 const float *gamma, const float *beta, float eps, void *u, void *sum, float *mean, float *rstd,
@@ -302,15 +331,15 @@ swimba_status launch_layer_norm_bwd(int64_t tokens, int D, int io_dtype, int res
                                     const float *gamma, const float *mean, const float *rstd, const void *d_sum, void *dx,
                                     void *dx_io, float *dgamma, float *dbeta, float *part, hipStream_t st)
 {
-    const bool sums = dgamma || dbeta;
+    const int64_t blocks = bwd_blocks(tokens, D);
+    const bool join = blocks != 1 && (dgamma || dbeta);
     if (tokens > 0) {
         const auto go = io_dtype == SWIMBA_F32 ? norm_bwd<float, float> : res_dtype == SWIMBA_F32 ? norm_bwd<bf16, float> : norm_bwd<bf16, bf16>;
-        const swimba_status s = go(tokens, D, du, r, gamma, mean, rstd, d_sum, dx, dx_io, sums ? part : nullptr, st);
+        const swimba_status s = go(tokens, D, du, r, gamma, mean, rstd, d_sum, dx, dx_io, join ? part : dgamma, join ? part + D : dbeta, st);
         if (s != SWIMBA_OK) return s;
     }
-    if (sums) {
-        hipLaunchKernelGGL(norm_reduce_kernel, dim3((unsigned)((2 * D + 31) / 32)), dim3(512), 0, st, part,
-                           (int)bwd_blocks(tokens, D), D, dgamma, dbeta);
+    if (join) {
+        hipLaunchKernelGGL(norm_reduce_kernel, dim3((unsigned)((2 * D + 31) / 32)), dim3(512), 0, st, part, (int)blocks, D, dgamma, dbeta);
         SWIMBA_CHECK_LAUNCH();
     }
     return SWIMBA_OK;

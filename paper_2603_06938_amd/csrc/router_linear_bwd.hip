@@ -266,7 +266,7 @@ Shares shares_of(int64_t tokens, int64_t per_share, int64_t step, int64_t want)
 }
 int experts_of(int E) { return E <= 16 ? 16 : E <= 32 ? 32 : 64; }                 // of a block of dW
 // Blocks that the chip holds at once at the kernels' registers, half of them for each product.
-int64_t blocks_of(int E) { return E <= 32 ? 512 : 256; }
+int64_t blocks_of(int E) { return E <= 16 ? 384 : E <= 32 ? 512 : 256; }
 int64_t dw_per_share(int D, int E) { return (int64_t)((D + LB_COLS - 1) / LB_COLS) * ((E + experts_of(E) - 1) / experts_of(E)); }
 // (in steps of bf16 tokens, of which those of fp32 are half: the shares do not depend on the type)
 Shares dw_shares(int64_t tokens, int D, int E) { return shares_of(tokens, dw_per_share(D, E), dw_step<bf16>() * LB_WAVES, blocks_of(E)); }
