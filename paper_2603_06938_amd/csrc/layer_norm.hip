@@ -12,6 +12,9 @@ namespace swimba {
 constexpr int norm_threads(int LPR) { return LPR < 256 ? 256 : LPR; }
 constexpr int rows_per_block(int LPR) { return norm_threads(LPR) / LPR; }
 
+// Threads of a block of the backward pass, of which two fit on a compute unit at the registers that its pieces take.
+constexpr int bwd_threads(int LPR, int NV) { return LPR > 64 ? LPR : NV == 1 ? 1024 : NV == 2 ? 512 : 256; }
+
 // sums of N values over the row's lanes, in every one of them; `round` alternates, so that one barrier a round is enough
 template <int LPR, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[N][16], int round)
@@ -118,12 +121,12 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
 
 // The blocks keep sums of their own for dgamma and dbeta: part (blocks, 2, D), or the two themselves where there is one block.
 template <typename T, typename R, int W, int NV, int LPR, bool TAIL>
-__global__ void __launch_bounds__(norm_threads(LPR))
+__global__ void __launch_bounds__(bwd_threads(LPR, NV))
 norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *__restrict__ gamma,
                 const float *__restrict__ mean, const float *__restrict__ rstd, const R *d_sum, R *dx, T *__restrict__ dx_io,
                 float *__restrict__ pgamma, float *__restrict__ pbeta, int64_t tokens, int D)
 {
-    constexpr int RPB = rows_per_block(LPR), SPAN = LPR * W;
+    constexpr int THREADS = bwd_threads(LPR, NV), RPB = THREADS / LPR, SPAN = LPR * W;
     constexpr bool AHEAD = LPR < 1024;                         // 1024 threads have no registers for it, nor for the gain
     __shared__ float lds[2][2][16];
     __shared__ float comb[RPB > 1 ? RPB * 2 * NV * SPAN : 1];
@@ -214,7 +217,7 @@ norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *
                 comb[(slot * 2 + 1) * NV * SPAN + d] = db[i][j];
             }
         __syncthreads();
-        for (int c = threadIdx.x; c < 2 * D; c += norm_threads(LPR)) {
+        for (int c = threadIdx.x; c < 2 * D; c += THREADS) {
             const int at = c < D ? c : c - D + NV * SPAN;
             float s = 0.f;
 #pragma unroll
@@ -304,7 +307,7 @@ swimba_status norm_fwd(int64_t tokens, int D, const void *x, const void *residua
 // its rows.
 int64_t bwd_blocks(int64_t tokens, int D)
 {
-    const int rpb = rows_per_block(lanes_per_row(D));
+    const int lpr = lanes_per_row(D), rpb = bwd_threads(lpr, (D + 4 * lpr - 1) / (4 * lpr)) / lpr;
     return tokens <= 4 * rpb ? (tokens > 0) : blocks_for(tokens, rpb, lanes_per_row(D) == 1024 ? 256 : 512);
 }
 
@@ -314,7 +317,7 @@ swimba_status norm_bwd(int64_t tokens, int D, const void *du, const void *r, con
 {
     auto go = [&](auto w, auto nv, auto lpr, auto tail) {
         hipLaunchKernelGGL((norm_bwd_kernel<T, R, w(), nv(), lpr(), tail()>), dim3((unsigned)bwd_blocks(tokens, D)),
-                           dim3(norm_threads(lpr)), 0, st, (const T *)du, (const R *)r, gamma, mean, rstd, (const R *)d_sum, (R *)dx,
+                           dim3(bwd_threads(lpr, nv)), 0, st, (const T *)du, (const R *)r, gamma, mean, rstd, (const R *)d_sum, (R *)dx,
                            (T *)dx_io, pgamma, pbeta, tokens, D);
     };
     with_row<T, R>(D, go);
