@@ -139,6 +139,7 @@ __device__ __forceinline__ uint32_t over_group(uint32_t v, Op op)
 }
 __device__ __forceinline__ uint32_t add_f32(uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }
 __device__ __forceinline__ uint32_t max_f32(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+__device__ __forceinline__ uint32_t add_u32(uint32_t a, uint32_t b) { return a + b; }
 __device__ __forceinline__ uint32_t or_u32(uint32_t a, uint32_t b) { return a | b; }
 template <int G> __device__ __forceinline__ float group_sum(float v) { return __uint_as_float(over_group<G>(__float_as_uint(v), add_f32)); }
 
