@@ -88,11 +88,15 @@ template <typename T, int NP, int G, bool FULL> struct Token {
         return last + 1 + over([&](int i, int j) { return key[i][j] - from; }, umin);
     }
 
-    // The K picks: lane l keeps the experts of rounds l, l + G, ...
-    __device__ __forceinline__ void picks(int K, int (&e)[SLOTS]) const
+    __device__ __forceinline__ bool names(uint32_t k) const { return k != NONE && (int)(k & LOW) < E; }
+    static __device__ __forceinline__ bool near(uint32_t a, uint32_t b) { return ((a ^ b) & ~LOW) == 0; }
+
+    // The K picks: lane l keeps the experts of rounds l, l + G, ... and, of bf16, their logits.  Of fp32 logits, whether some agree
+    // in their keys' upper bits, down to the pick behind the last, which is `behind` (-1: there is none).
+    __device__ __forceinline__ bool picks(int K, int (&e)[SLOTS], float (&v)[SLOTS], int &behind) const
     {
         uint32_t b = best;
-        bool close = false;
+        bool close = false, end = false;
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i) {
             uint32_t mine = 0;
@@ -100,35 +104,76 @@ template <typename T, int NP, int G, bool FULL> struct Token {
 #pragma unroll 1
             for (int r = 0; r < rounds; ++r) {
                 mine = l == r ? b : mine;
-                if (BF && i * G + r == K - 1) break;           // the pick behind the last shows whether fp32 ones are close
+                if (BF && i * G + r == K - 1) break;
                 const uint32_t n = next(b);
-                if (!BF) close = close || ((b ^ n) & ~LOW) == 0;
+                if (!BF) {
+                    end = n > b && near(b, n);
+                    close = close || end;
+                    if (i * G + r == K - 1) behind = n > b && names(n) ? (int)(n & LOW) : -1;
+                }
                 b = n;
             }
             e[i] = mine & LOW;
+            v[i] = BF ? at_place(mine >> 16) : 0.f;
         }
         if constexpr (!BF) {
-            if (__any(close)) {                                // whole places, equal ones by the expert
-                uint32_t last = 0;
-                int x = -1;
-                auto place = [&](int i, int j) { return place_of(p[i].get(j)); };
-#pragma unroll
-                for (int i = 0; i < SLOTS; ++i) {
-                    const int rounds = min(K - i * G, G);
-#pragma unroll 1
-                    for (int r = 0; r < rounds; ++r) {
-                        auto behind = [&](int q, int j) {
-                            const uint32_t o = place(q, j);
-                            return real(q, j) && (o > last || (o == last && expert(q, j) > x));
-                        };
-                        const uint32_t o = over([&](int q, int j) { return behind(q, j) ? place(q, j) : NONE; }, umin);
-                        x = (int)over([&](int q, int j) { return behind(q, j) && place(q, j) == o ? (uint32_t)expert(q, j) : 1u << 20; }, umin);
-                        last = o;
-                        e[i] = l == r ? x : e[i];
-                    }
-                }
+            // agreement that goes on behind that pick leaves the choice to exact()
+            if (__any(end) && end && behind >= 0) {
+                const uint32_t n = next(b);
+                if (n > b && near(b, n)) behind = -2;
             }
         }
+        return close;
+    }
+    // the same by whole places, equal ones by the expert
+    __device__ __forceinline__ void exact(int K, int (&e)[SLOTS]) const
+    {
+        uint32_t last = 0;
+        int x = -1;
+        auto place = [&](int i, int j) { return place_of(p[i].get(j)); };
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            const int rounds = min(K - i * G, G);
+#pragma unroll 1
+            for (int r = 0; r < rounds; ++r) {
+                auto after = [&](int q, int j) {
+                    const uint32_t o = place(q, j);
+                    return real(q, j) && (o > last || (o == last && expert(q, j) > x));
+                };
+                const uint32_t o = over([&](int q, int j) { return after(q, j) ? place(q, j) : NONE; }, umin);
+                x = (int)over([&](int q, int j) { return after(q, j) && place(q, j) == o ? (uint32_t)expert(q, j) : 1u << 20; }, umin);
+                last = o;
+                e[i] = l == r ? x : e[i];
+            }
+        }
+    }
+    // Where the picks that lie in the lanes, and the one behind them, stand among themselves by whole places: rank[i] of the lane's
+    // own, the result that of the one behind.
+    __device__ __forceinline__ int rank_of(int K, const int (&e)[SLOTS], const float (&v)[SLOTS], int behind, float vb, int (&rank)[SLOTS]) const
+    {
+        const int from = (threadIdx.x & 63) - l;
+        uint32_t mine[SLOTS];
+        int over_b = 0;
+        const uint32_t pb = behind >= 0 ? place_of(vb) : NONE;
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) {
+            mine[i] = place_of(v[i]);
+            rank[i] = pb < mine[i] || (pb == mine[i] && behind < e[i]);
+            rank[i] = behind >= 0 ? rank[i] : 0;
+        }
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q) {
+            const int rounds = min(K - q * G, G);
+#pragma unroll 1
+            for (int r = 0; r < rounds; ++r) {
+                const uint32_t o = (uint32_t)__shfl((int)mine[q], from + r);
+                const int x = __shfl(e[q], from + r);
+#pragma unroll
+                for (int i = 0; i < SLOTS; ++i) rank[i] += o < mine[i] || (o == mine[i] && x < e[i]);
+                over_b += o < pb || (o == pb && x < behind);
+            }
+        }
+        return behind >= 0 ? over_b : K;
     }
 };
 
@@ -203,8 +248,22 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
         } else
             fetch(s, t);
         const Tok tok(s.p, l, E);
-        int e[Tok::SLOTS];
-        tok.picks(K, e);
+        const int64_t row = grp * tokens + (t + at < tokens ? t + at : tokens - 1);
+        int e[Tok::SLOTS], rank[Tok::SLOTS], behind = -1, rank_b = K;
+        float v[Tok::SLOTS];
+        const bool close = tok.picks(K, e, v, behind);
+        if (!Tok::BF && __any(behind == -2)) {
+            tok.exact(K, e);
+            behind = -1;
+        }
+#pragma unroll
+        for (int i = 0; i < Tok::SLOTS; ++i) {
+            rank[i] = i * G + l;
+            if (!Tok::BF && rank[i] < K) v[i] = to_float(logits[row * E + e[i]]);      // its key does not hold the whole of it
+        }
+        if constexpr (!Tok::BF) {
+            if (__any(close)) rank_b = tok.rank_of(K, e, v, behind, to_float(logits[row * E + (behind >= 0 ? behind : 0)]), rank);
+        }
         const float m = tok.top;
         bool on = s.on;
         if (__any(m == -INFINITY)) {                           // a token whose logits are all -inf does not count
@@ -236,16 +295,15 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
             for (int j = 0; j < 8; ++j) Z += p[i][j];
         const float invZ = 1.0f / group_sum<G>(Z);
         if (t + at < tokens) {
-            const int64_t row = grp * tokens + t + at;
+            auto put = [&](int r, int x, float f) __attribute__((always_inline)) {
+                if (topk_idx) topk_idx[row * K + r] = x;
+                if (topk_w) topk_w[row * K + r] = route_exp(f - m) * invZ;
+                if (on) atomicAdd(&csum[x], 1);                // whole numbers: the order does not matter
+            };
 #pragma unroll
-            for (int i = 0; i < Tok::SLOTS; ++i) {
-                const int r = i * G + l;
-                if (r < K) {
-                    if (topk_idx) topk_idx[row * K + r] = e[i];
-                    if (topk_w) topk_w[row * K + r] = route_exp(to_float(logits[row * E + e[i]]) - m) * invZ;
-                    if (on) atomicAdd(&csum[e[i]], 1);         // whole numbers: the order does not matter
-                }
-            }
+            for (int i = 0; i < Tok::SLOTS; ++i)
+                if (i * G + l < K && rank[i] < K) put(rank[i], e[i], v[i]);
+            if (!Tok::BF && l == 0 && rank_b < K) put(rank_b, behind, to_float(logits[row * E + behind]));
         }
         if (on) {
 #pragma unroll

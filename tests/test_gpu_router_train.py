@@ -94,6 +94,25 @@ def test_masked_logits(E, k, io):
     assert (got[:, 3::11] == 0).all()
 
 
+@pytest.mark.parametrize("E,k", EXPERTS)
+def test_logits_that_differ_in_their_last_bits(E, k):
+    """fp32 logits in runs that differ by a few of their lowest bits, and equal ones among them: pairs, runs across the last
+    pick, whole tokens; positive, negative and across zero."""
+    gen = torch.Generator().manual_seed(E)
+    L = 400
+    base = torch.randint(0, max(2, E // 2), (1, L, E), generator=gen)          # members of one run share a number
+    base[:, ::5] = torch.randint(0, E, (1, L // 5, E), generator=gen)
+    base[:, ::7] = 0
+    sign = torch.where(torch.arange(L) % 3 == 0, -1.0, 1.0)[None, :, None]
+    z = sign * (1.0 + base / 16)
+    bits = z.float().view(torch.int32) + torch.randint(0, 300, (1, L, E), generator=gen, dtype=torch.int32) // torch.tensor([1, 40, 300])[torch.arange(L) % 3][None, :, None]
+    z = bits.int().view(torch.float32)
+    z[:, 3::11] -= 1.0
+    z = z.to("cuda:0")
+    out = sw.swimba_router_balance(z, k)
+    check_balance(z, k, None, False, out)
+
+
 @pytest.mark.parametrize("E,k", [(8, 2), (64, 4), (100, 2)])
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_padding_holds_anything(E, k, io):
