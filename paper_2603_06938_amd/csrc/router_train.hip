@@ -332,24 +332,25 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
     else if (x < E) part[(int64_t)blockIdx.x * E + x] = make_float2(v, __int_as_float(c));
 }
 
-// The slices of a group joined, 32 experts to a block of 1024 threads: 32 half waves take every 32nd slice each.  The block that
-// is done last (a ticket that balance_kernel has set to zero) finishes the loss; what it adds up has an order of its own, so
-// that it does not matter which one that is.
+// The slices of a group joined, 64 experts to a block of 1024 threads: 16 waves take every 16th slice each.  Of several blocks
+// the one that is done last (a ticket that balance_kernel has set to zero) finishes the loss; what it adds up has an order of
+// its own, so that it does not matter which one that is.
+constexpr int LOSS_EXPERTS = 64;
 __global__ void __launch_bounds__(1024)
 balance_loss_kernel(const float2 *__restrict__ part, int slices, int E, int K, int32_t *counts, float *__restrict__ prob_mean,
                     float *__restrict__ loss, float *psums, int *ticket)
 {
-    __shared__ float2 lds[32][33];
+    __shared__ float2 lds[16][LOSS_EXPERTS];
     __shared__ double fin[2][4];
     __shared__ bool last;
-    const int blocks = (E + 31) / 32;
+    const int blocks = (E + LOSS_EXPERTS - 1) / LOSS_EXPERTS;
     const int64_t grp = blockIdx.x / blocks;
-    const int col = threadIdx.x % 32, row = threadIdx.x / 32, e = blockIdx.x % blocks * 32 + col;
+    const int col = threadIdx.x % LOSS_EXPERTS, row = threadIdx.x / LOSS_EXPERTS, e = blockIdx.x % blocks * LOSS_EXPERTS + col;
     int c = 0;
     float p = 0.f;
     if (e < E) {
-#pragma unroll 8
-        for (int s = row; s < slices; s += 32) {
+#pragma unroll 16
+        for (int s = row; s < slices; s += 16) {
             const float2 v = part[(grp * slices + s) * E + e];
             p += v.x;
             c += __float_as_int(v.y);
@@ -359,11 +360,13 @@ balance_loss_kernel(const float2 *__restrict__ part, int slices, int E, int K, i
     __syncthreads();
     p = 0.f;
     c = 0;
-    if (row == 0)
-        for (int i = 0; i < 32; ++i) {
+    if (row == 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
             p += lds[i][col].x;
             c += __float_as_int(lds[i][col].y);
         }
+    }
     if (blocks > 1) {
         if (row == 0 && e < E) {
             __hip_atomic_store(psums + grp * E + e, p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -465,7 +468,7 @@ swimba_status launch_router_balance(int64_t groups, int64_t tokens, int E, int K
     });
     SWIMBA_CHECK_LAUNCH();
     if (s.count > 1) {
-        hipLaunchKernelGGL(balance_loss_kernel, dim3((unsigned)(groups * ((E + 31) / 32))), dim3(1024), 0, st, part, (int)s.count, E, K,
+        hipLaunchKernelGGL(balance_loss_kernel, dim3((unsigned)(groups * ((E + LOSS_EXPERTS - 1) / LOSS_EXPERTS))), dim3(1024), 0, st, part, (int)s.count, E, K,
                            counts, prob_mean, loss, psums, ticket);
         SWIMBA_CHECK_LAUNCH();
     }
