@@ -220,3 +220,44 @@ def test_on_another_stream_and_from_a_graph():
         graphs[rep & 1].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), rep
+
+
+def test_more_than_2_to_the_31_elements():
+    """Rows past the 2^31st and the 2^32nd byte are found: the last ones against their formulas, the sums over all of them."""
+    T, D = 140000, 16384
+    x = torch.zeros(T, D, dtype=torch.bfloat16, device="cuda:0")
+    spots = [0, 65535, 131071, 131072, 135000, T - 1]
+    gen = torch.Generator("cuda:0").manual_seed(3)
+    for t in spots:
+        x[t] = torch.randn(D, device="cuda:0", generator=gen) + 1
+    gamma, beta = torch.randn(D, device="cuda:0", generator=gen), torch.randn(D, device="cuda:0", generator=gen)
+    out = sw.swimba_layer_norm(x, gamma, beta, 1e-5, want_stats=True)
+    at = torch.tensor(spots, device="cuda:0")
+    check_fwd(x[at], None, gamma, beta, 1e-5, sw.NormOut(out.u[at], None, out.mean[at], out.rstd[at]))
+    assert torch.equal(out.u[T - 2], beta.bfloat16())
+    du = torch.zeros_like(x)
+    du[at] = x[at] * 0.5
+    got = sw.swimba_layer_norm_bwd(du, x, gamma, out.mean, out.rstd)
+    (rx, rg, rb), (bx, bg, bb) = norm_bwd(du[at], x[at], gamma, out.mean[at], out.rstd[at])
+    within(got.dx[at], rx, bx + half(x.dtype) * (rx.abs() + bx), "dx")
+    within(got.dgamma, rg, bg, "dgamma")                       # the rows of zeros add nothing
+    within(got.dbeta, rb, bb, "dbeta")
+    assert (got.dx[T - 2] == 0).all()
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each."""
+    a, b = [case(3000, 700, "bf16", "f32", s) for s in (1, 2)]
+    one = [sw.swimba_layer_norm(x, g, w, 1e-5, r, want_stats=True) for x, r, g, w in (a, b)]
+    want = [sw.swimba_layer_norm_bwd(c[0], o.sum, c[2], o.mean, o.rstd, c[1]) for c, o in zip((a, b), one)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for rep in range(3):
+        got = []
+        for s, c in zip(streams, (a, b)):
+            with torch.cuda.stream(s):
+                o = sw.swimba_layer_norm(c[0], c[2], c[3], 1e-5, c[1], want_stats=True)
+                got.append((o, sw.swimba_layer_norm_bwd(c[0], o.sum, c[2], o.mean, o.rstd, c[1])))
+        torch.cuda.synchronize()
+        for (o, g), w, o1 in zip(got, want, one):
+            assert torch.equal(o.u, o1.u) and all(torch.equal(p, q) for p, q in zip(g, w))

@@ -400,3 +400,113 @@ def test_a_training_step_replays_from_graphs(io):
         graphs[rep & 1].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs[rep & 1], want)), rep
+
+
+def test_more_than_2_to_the_31_logits():
+    """Tokens past the 2^31st logit and the 2^32nd byte: the last ones against their formulas, and every token counted."""
+    T, E, k = 8388608 + 70000, 256, 2
+    z = torch.empty(1, T, E, dtype=torch.bfloat16, device="cuda:0")
+    z[0, :4096].normal_(generator=torch.Generator("cuda:0").manual_seed(1))
+    for a in range(4096, T, 4096):                             # the same tokens over and over, the last ones others
+        n = min(4096, T - a)
+        z[0, a:a + n] = z[0, :n]
+    z[0, -100:].normal_(generator=torch.Generator("cuda:0").manual_seed(2))
+    out = sw.swimba_router_balance(z, k)
+    tail = z[:, -100:].contiguous()
+    assert torch.equal(out.topk_idx[0, -100:].cpu().long(), picks(tail, k)[0])
+    first = torch.bincount(picks(z[:, :4096], k).reshape(-1), minlength=E)
+    whole, rest = divmod(T, 4096)
+    want = whole * first + torch.bincount(picks(z[:, :rest], k).reshape(-1), minlength=E)
+    want += torch.bincount(picks(tail, k).reshape(-1), minlength=E) - torch.bincount(picks(z[:, rest - 100:rest], k).reshape(-1), minlength=E)
+    assert torch.equal(out.counts[0].cpu().long(), want) and int(out.counts.sum()) == k * T
+    dw = torch.zeros(1, T, k, device="cuda:0")
+    dw[0, -100:] = 1.0
+    dw[0, -50, 1] = -3.0
+    got = sw.swimba_router_bwd(z, out.topk_idx, dw)
+    ref, bound = routing_bwd(tail, out.topk_idx[:, -100:].contiguous(), dw[:, -100:].contiguous(), None, None)
+    within(got[:, -100:], ref, bound + half(z.dtype) * (ref.abs() + bound), "d_logits")
+    assert (got[0, :-100] == 0).all()
+
+
+def test_more_than_2_to_the_31_features():
+    T, D, E = 270000, 8192, 8
+    u = torch.zeros(T, D, dtype=torch.bfloat16, device="cuda:0")
+    g = torch.zeros(T, E, dtype=torch.bfloat16, device="cuda:0")
+    spots = torch.tensor([0, 131071, 131072, 262143, 262144, 269000, T - 1], device="cuda:0")
+    gen = torch.Generator("cuda:0").manual_seed(3)
+    u[spots] = torch.randn(7, D, device="cuda:0", generator=gen).bfloat16()
+    g[spots] = torch.randn(7, E, device="cuda:0", generator=gen).bfloat16()
+    W = torch.randn(E, D, device="cuda:0", generator=gen).bfloat16()
+    out = sw.swimba_router_linear_bwd(u, W, g, u)
+    (du, dW), (bu, bw) = linear_bwd(u[spots], W, g[spots], u[spots])
+    within(out.du[spots], du, bu + half(u.dtype) * (du.abs() + bu), "du")
+    within(out.dW_g, dW, bw, "dW_g")
+    assert (out.du[T - 2] == 0).all()
+
+
+def test_two_steps_at_once():
+    """Two streams; every call has a workspace of its own."""
+    steps = [Step(2, 3000, 256, 72, 4, "bf16", s) for s in (1, 2)]
+    want = [s.run() for s in steps]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for rep in range(3):
+        got = []
+        for st, s in zip(streams, steps):
+            with torch.cuda.stream(st):
+                got.append(s.run())
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(p, q) for p, q in zip(a, b)), rep
+
+
+def test_every_argument_is_checked():
+    """A tensor of another type, shape, layout or device is named and refused."""
+    dev = "cuda:0"
+    f = lambda *s, dtype=torch.float32: torch.ones(*s, dtype=dtype, device=dev)
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device=dev)
+    bf = torch.bfloat16
+    calls = {
+        "swimba_layer_norm": (dict(x=f(2, 3, 8, dtype=bf), gamma=f(8), beta=f(8), eps=1e-5, residual=f(2, 3, 8), u=f(2, 3, 8, dtype=bf),
+                                   sum=f(2, 3, 8), mean=f(2, 3), rstd=f(2, 3)), "x gamma beta residual u sum mean rstd"),
+        "swimba_layer_norm_bwd": (dict(du=f(2, 3, 8, dtype=bf), r=f(2, 3, 8), gamma=f(8), mean=f(2, 3), rstd=f(2, 3), d_sum=f(2, 3, 8),
+                                       dx=f(2, 3, 8), dx_io=f(2, 3, 8, dtype=bf), dgamma=f(8), dbeta=f(8)),
+                                  "du r gamma mean rstd d_sum dx dx_io dgamma dbeta"),
+        "swimba_router_balance": (dict(router_logits=f(2, 3, 8), top_k=2, mask=torch.ones(2, 3, dtype=torch.bool, device=dev), loss=f(1),
+                                       counts=i32(1, 8), prob_mean=f(1, 8), topk_idx=i32(2, 3, 2), topk_w=f(2, 3, 2)),
+                                  "router_logits mask loss counts prob_mean topk_idx topk_w"),
+        "swimba_router_bwd": (dict(router_logits=f(2, 3, 8), topk_idx=i32(2, 3, 2), d_topk_w=f(2, 3, 2), counts=i32(2, 8), d_loss=f(2),
+                                   mask=torch.ones(2, 3, dtype=torch.uint8, device=dev), d_logits=f(2, 3, 8)),
+                              "router_logits topk_idx d_topk_w counts d_loss mask d_logits"),
+        "swimba_router_linear_bwd": (dict(u=f(2, 3, 8), W_g=f(4, 8), d_logits=f(2, 3, 4), du_add=f(2, 3, 8), du=f(2, 3, 8), dW_g=f(4, 8)),
+                                     "u W_g d_logits du_add du dW_g"),
+    }
+    for call, (args, names) in calls.items():
+        getattr(sw, call)(**args)
+        for name in names.split():
+            t = args[name]
+            wrong = [t.double(), t.cpu(), torch.cat([t, t], -1), [1.0]]
+            if t.numel() > 1:
+                wrong.append(torch.stack([t, t], -1)[..., 0])              # not contiguous
+            for w in wrong:
+                if name in ("x", "du", "router_logits", "u") and w is wrong[2]:
+                    continue                                   # the sizes are read from it: another argument is refused then
+                with pytest.raises((TypeError, ValueError)):
+                    getattr(sw, call)(**dict(args, **{name: w}))
+    with pytest.raises(ValueError):
+        sw.swimba_layer_norm(f(2, 8), sum=f(2, 8))
+    with pytest.raises(ValueError):
+        sw.swimba_layer_norm_bwd(f(2, 8), f(2, 8), None, f(2), f(2), dx_io=f(2, 8))
+    with pytest.raises(TypeError):
+        sw.swimba_layer_norm(f(2, 8), residual=f(2, 8, dtype=bf))
+    with pytest.raises(sw.SwimbaError):
+        sw.swimba_layer_norm(f(2, 8), eps=0.0)
+    with pytest.raises(sw.SwimbaError):
+        sw.swimba_router_linear_bwd(f(2, 8), f(300, 8), f(2, 300))
+    with pytest.raises(sw.SwimbaError):
+        short = sw.swimba_router_linear_bwd_workspace_bytes(2000, 8, 4) - 1
+        sw.swimba_router_linear_bwd(f(2000, 8), f(4, 8), f(2000, 4), workspace=torch.empty(short, dtype=torch.uint8, device=dev))
+    with pytest.raises(ValueError):
+        sw.swimba_router_balance(f(8, 4), 2, per_sequence=True)
+    with pytest.raises(ValueError):
+        sw.swimba_router_balance(f(8, 4), 1 << 32)
