@@ -126,7 +126,8 @@ def main() -> int:
     ap.add_argument("--no-decode", action="store_true")
     ap.add_argument("--no-others", action="store_true", help="skip the other prefill workloads")
     ap.add_argument("--proj", type=int, default=0, metavar="D_MODEL",
-                    help="also time the routed expert in-projection from token features of this width")
+                    help="also time the routed expert in-projection from token features of this width, and the calls "
+                         "that train the routing on them")
     ap.add_argument("--xe", action="store_true",
                     help="also time the forward with one input stream per expert (rank-k injection)")
     ap.add_argument("--contrast", action="store_true",
@@ -586,7 +587,36 @@ def main() -> int:
             "ms": round(xms, 5), "mfma_TFLOPs": round(xflops / xms / 1e9, 1),
             "mfma_frac": round(xflops / xms / 1e9 / PEAK_BF16_TFLOPS, 4),
             "features_to_y_ms": round(fxms, 5), "tokens_per_s": round(T / fxms * 1e3, 1)}
+        # training the routing on the same features: norm (into an fp32 residual stream), router, routing with the balance
+        # loss of each sequence, and back through all of them
+        gain, bias = torch.ones(Dm, device=dev), torch.zeros(Dm, device=dev)
+        stream = torch.randn((w.batch, w.seqlen, Dm), generator=gen, device=dev)
+        d_w = torch.randn((w.batch, w.seqlen, k), generator=gen, device=dev) / T
+        d_loss = torch.full((w.batch,), 0.01 / w.batch, device=dev)
+        norm = sw.swimba_layer_norm(us[0], gain, bias, 1e-5, stream, want_stats=True)
+        route = sw.swimba_router_balance(sw.swimba_router_linear(norm.u, Wg), k, per_sequence=True)
+        d_lg = sw.swimba_router_bwd(lg, route.topk_idx, d_w, route.counts, d_loss)
+        back = sw.swimba_router_linear_bwd(norm.u, Wg, d_lg)
+
+        def routing_step(i):
+            n = sw.swimba_layer_norm(us[i % 3], gain, bias, 1e-5, stream, want_stats=True)
+            sw.swimba_router_linear(n.u, Wg, lg)
+            b = sw.swimba_router_balance(lg, k, per_sequence=True)
+            dz = sw.swimba_router_bwd(lg, b.topk_idx, d_w, b.counts, d_loss)
+            g = sw.swimba_router_linear_bwd(n.u, Wg, dz)
+            sw.swimba_layer_norm_bwd(g.du, n.sum, gain, n.mean, n.rstd)
+
+        proj_res["routing_training"] = {"what": "norm -> router -> routing with a balance loss, forward and backward"}
+        for name, fn in (("layer_norm_ms", lambda i: sw.swimba_layer_norm(us[i % 3], gain, bias, 1e-5, stream, want_stats=True)),
+                         ("router_balance_ms", lambda i: sw.swimba_router_balance(lg, k, per_sequence=True)),
+                         ("router_bwd_ms", lambda i: sw.swimba_router_bwd(lg, route.topk_idx, d_w, route.counts, d_loss)),
+                         ("router_linear_bwd_ms", lambda i: sw.swimba_router_linear_bwd(us[i % 3], Wg, d_lg)),
+                         ("layer_norm_bwd_ms", lambda i: sw.swimba_layer_norm_bwd(back.du, norm.sum, gain, norm.mean, norm.rstd)),
+                         ("step_ms", routing_step)):
+            time_loop(fn, 3)
+            proj_res["routing_training"][name] = round(time_loop(fn, K), 5)
         # the projection overwrote the synthetic expert rows of every set with its own values
+        del stream, norm, route, back, d_w, d_lg
         del us, WBs, WCs, WXs, pws, fws, xpw, xfw
 
     # ---- one input stream per expert (rank-k injection) -------------------------------------------
