@@ -430,6 +430,7 @@ swimba_status swimba_layer_norm(int64_t tokens, int32_t d_model, int32_t io_dtyp
  *   dgamma, dbeta (d_model) fp32 [out]     NULL = not wanted
  * The sums over the tokens are taken in fp32 in an order that sizes alone decide (zero for no tokens).
  *   workspace >= swimba_layer_norm_bwd_workspace_bytes(tokens, d_model), 256-byte aligned.
+ *            Where that is 256, its smallest, nothing is kept there and it may be NULL.
  */
 size_t swimba_layer_norm_bwd_workspace_bytes(int64_t tokens, int32_t d_model);
 swimba_status swimba_layer_norm_bwd(int64_t tokens, int32_t d_model, int32_t io_dtype, int32_t res_dtype, const void *du,
@@ -455,6 +456,7 @@ swimba_status swimba_layer_norm_bwd(int64_t tokens, int32_t d_model, int32_t io_
  * At most 2^31 - 1 tokens to a group and 2^38 in all.  Element-aligned pointers; rows of logits that start 16-byte
  * aligned (by pointer and E) are read in larger pieces.
  *   workspace >= swimba_router_balance_workspace_bytes(groups, tokens, nexperts), 256-byte aligned.
+ *            Where that is 256, its smallest, nothing is kept there and it may be NULL.
  */
 size_t swimba_router_balance_workspace_bytes(int64_t groups, int64_t tokens, int32_t nexperts);
 swimba_status swimba_router_balance(int64_t groups, int64_t tokens, int32_t nexperts, int32_t top_k, int32_t io_dtype,
@@ -490,6 +492,7 @@ swimba_status swimba_router_bwd(int64_t groups, int64_t tokens, int32_t nexperts
  * u is read for dW_g only, W_g for du only; the other may be NULL.  Limits, alignment (du, du_add as u) and the
  * element-wise reading of rows that are no multiple of 16 bytes as in swimba_router_linear; dW_g by element.
  *   workspace >= swimba_router_linear_bwd_workspace_bytes(tokens, d_model, nexperts), 256-byte aligned.
+ *            Where that is 256, its smallest, nothing is kept there and it may be NULL.
  */
 size_t swimba_router_linear_bwd_workspace_bytes(int64_t tokens, int32_t d_model, int32_t nexperts);
 swimba_status swimba_router_linear_bwd(int64_t tokens, int32_t d_model, int32_t nexperts, int32_t io_dtype, const void *u,

@@ -335,6 +335,13 @@ swimba_status swimba_router_linear(int64_t tokens, int32_t d_model, int32_t nexp
 }
 
 // ---- what trains the routing --------------------------------------------------------------
+// Sizes of workspaces that a call may do without: 256 where nothing is kept in one, more where something is.
+static size_t optional_workspace(size_t need) { return need > 0 ? align_up(need > 256 ? need : 257, 256) : 256; }
+static bool bad_workspace(size_t need, const void *workspace, size_t bytes)
+{
+    return need > 0 && (!workspace || bytes < optional_workspace(need) || ((uintptr_t)workspace & 255u));
+}
+
 static swimba_status check_norm(int64_t tokens, int32_t d_model)
 {
     if (tokens < 0 || d_model < 1) return SWIMBA_ERR_SHAPE;
@@ -367,8 +374,7 @@ swimba_status swimba_layer_norm(int64_t tokens, int32_t d_model, int32_t io_dtyp
 size_t swimba_layer_norm_bwd_workspace_bytes(int64_t tokens, int32_t d_model)
 {
     if (check_norm(tokens, d_model) != SWIMBA_OK) return 0;
-    const size_t n = layer_norm_bwd_bytes(tokens, d_model);
-    return align_up(n > 0 ? n : 1, 256);
+    return optional_workspace(layer_norm_bwd_bytes(tokens, d_model));
 }
 
 swimba_status swimba_layer_norm_bwd(int64_t tokens, int32_t d_model, int32_t io_dtype, int32_t res_dtype, const void *du,
@@ -381,8 +387,7 @@ swimba_status swimba_layer_norm_bwd(int64_t tokens, int32_t d_model, int32_t io_
     if (dx_io && res_dtype == io_dtype) return SWIMBA_ERR_DTYPE;
     st = check_norm(tokens, d_model);
     if (st != SWIMBA_OK) return st;
-    if (!workspace || workspace_bytes < swimba_layer_norm_bwd_workspace_bytes(tokens, d_model) || ((uintptr_t)workspace & 255u))
-        return SWIMBA_ERR_WORKSPACE;
+    if (bad_workspace(layer_norm_bwd_bytes(tokens, d_model), workspace, workspace_bytes)) return SWIMBA_ERR_WORKSPACE;
     if (tokens > 0 && (!du || !r || !mean || !rstd || !dx)) return SWIMBA_ERR_NULL;
     if (check_align(io_dtype, {du, r, d_sum, dx, dx_io}, {}, {gamma, mean, rstd, dgamma, dbeta}) != SWIMBA_OK)
         return SWIMBA_ERR_ALIGNMENT;
@@ -409,8 +414,7 @@ static swimba_status check_routing(int64_t groups, int64_t tokens, int32_t nexpe
 size_t swimba_router_balance_workspace_bytes(int64_t groups, int64_t tokens, int32_t nexperts)
 {
     if (check_groups(groups, tokens, nexperts) != SWIMBA_OK) return 0;
-    const size_t n = balance_bytes(groups, tokens, nexperts);
-    return align_up(n > 0 ? n : 1, 256);
+    return optional_workspace(balance_bytes(groups, tokens, nexperts));
 }
 
 swimba_status swimba_router_balance(int64_t groups, int64_t tokens, int32_t nexperts, int32_t top_k, int32_t io_dtype,
@@ -421,9 +425,7 @@ swimba_status swimba_router_balance(int64_t groups, int64_t tokens, int32_t nexp
     swimba_status st = check_routing(groups, tokens, nexperts, top_k, io_dtype);
     if (st != SWIMBA_OK) return st;
     if (groups == 0) return SWIMBA_OK;
-    if (!workspace || workspace_bytes < swimba_router_balance_workspace_bytes(groups, tokens, nexperts) ||
-        ((uintptr_t)workspace & 255u))
-        return SWIMBA_ERR_WORKSPACE;
+    if (bad_workspace(balance_bytes(groups, tokens, nexperts), workspace, workspace_bytes)) return SWIMBA_ERR_WORKSPACE;
     if ((tokens > 0 && !logits) || !counts || !loss) return SWIMBA_ERR_NULL;
     if (check_align(io_dtype, {}, {logits}, {topk_idx, topk_w, counts, prob_mean, loss}) != SWIMBA_OK) return SWIMBA_ERR_ALIGNMENT;
     return launch_router_balance(groups, tokens, nexperts, top_k, io_dtype, logits, mask, topk_idx, topk_w, counts, prob_mean,
@@ -454,8 +456,7 @@ static swimba_status check_linear(int64_t tokens, int32_t d_model, int32_t nexpe
 size_t swimba_router_linear_bwd_workspace_bytes(int64_t tokens, int32_t d_model, int32_t nexperts)
 {
     if (check_linear(tokens, d_model, nexperts) != SWIMBA_OK) return 0;
-    const size_t n = router_linear_bwd_bytes(tokens, d_model, nexperts);
-    return align_up(n > 0 ? n : 1, 256);
+    return optional_workspace(router_linear_bwd_bytes(tokens, d_model, nexperts));
 }
 
 swimba_status swimba_router_linear_bwd(int64_t tokens, int32_t d_model, int32_t nexperts, int32_t io_dtype, const void *u,
@@ -465,9 +466,7 @@ swimba_status swimba_router_linear_bwd(int64_t tokens, int32_t d_model, int32_t 
     if (io_dtype != SWIMBA_F32 && io_dtype != SWIMBA_BF16) return SWIMBA_ERR_DTYPE;
     swimba_status st = check_linear(tokens, d_model, nexperts);
     if (st != SWIMBA_OK) return st;
-    if (!workspace || workspace_bytes < swimba_router_linear_bwd_workspace_bytes(tokens, d_model, nexperts) ||
-        ((uintptr_t)workspace & 255u))
-        return SWIMBA_ERR_WORKSPACE;
+    if (bad_workspace(router_linear_bwd_bytes(tokens, d_model, nexperts), workspace, workspace_bytes)) return SWIMBA_ERR_WORKSPACE;
     if (tokens > 0 && (!d_logits || (du && !W_g) || (dW_g && !u) || (du_add && !du))) return SWIMBA_ERR_NULL;
     if (check_align(io_dtype, {u, W_g, du_add, du}, {d_logits}, {dW_g}) != SWIMBA_OK) return SWIMBA_ERR_ALIGNMENT;
     return launch_router_linear_bwd(tokens, d_model, nexperts, io_dtype, u, W_g, d_logits, du_add, du, dW_g, workspace,

@@ -405,7 +405,7 @@ void take_on(Out &out, PyObject *given, bool wanted, const char *name, at::Scala
 
 Workspace workspace_on(PyObject *given, size_t want, at::Device dev)
 {
-    Workspace ws(given, want, dev);
+    Workspace ws(given, want == 256 ? 0 : want, dev);      // 256: the call keeps nothing there and takes none
     same_device(given, "workspace", dev);
     return ws;
 }

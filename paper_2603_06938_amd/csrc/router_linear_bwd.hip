@@ -310,7 +310,11 @@ swimba_status linear_bwd(int64_t tokens, int D, int E, const void *u, const void
 
 }  // namespace
 
-size_t router_linear_bwd_bytes(int64_t tokens, int D, int E) { return (size_t)dw_shares(tokens, D, E).count * E * D * sizeof(float); }
+size_t router_linear_bwd_bytes(int64_t tokens, int D, int E)
+{
+    const int64_t n = dw_shares(tokens, D, E).count;
+    return n > 1 ? (size_t)n * E * D * sizeof(float) : 0;
+}
 
 swimba_status launch_router_linear_bwd(int64_t tokens, int D, int E, int io_dtype, const void *u, const void *Wg, const void *dl,
                                        const void *du_add, void *du, float *dW, void *work, hipStream_t st)

@@ -409,7 +409,7 @@ Slices balance_slices(int64_t groups, int64_t tokens, int E, int element)
 {
     const int most = balance_most(pieces_of(E), element);
     const int64_t threads = tokens * routing_lanes_of(E), steps = (threads + most - 1) / most;
-    if (steps <= 4 || groups >= 256) {
+    if (steps <= 4 || groups >= 256 || groups == 0) {
         int n = 256;
         while (n < most && n < threads) n *= 2;
         return {n, 1};

@@ -26,7 +26,7 @@ def test_layer_norm(kw, status):
     assert norm(**kw) == status
 
 
-def norm_bwd(tokens=4, D=64, io=BF16, res=F32, du=P[0], r=P[1], gamma=P[2], mean=P[3], rstd=P[4], d_sum=P[5], dx=P[6], dx_io=P[7],
+def norm_bwd(tokens=400, D=64, io=BF16, res=F32, du=P[0], r=P[1], gamma=P[2], mean=P[3], rstd=P[4], d_sum=P[5], dx=P[6], dx_io=P[7],
              dgamma=P[8], dbeta=P[9], ws=P[10], size=None):
     lib = sw._load()
     size = lib.swimba_layer_norm_bwd_workspace_bytes(tokens, D) if size is None else size
@@ -46,7 +46,7 @@ def test_layer_norm_bwd(kw, status):
     assert norm_bwd(**kw) == status
 
 
-def balance(groups=2, tokens=5, E=8, k=2, io=BF16, logits=P[0], mask=P[1], idx=P[2], w=P[3], counts=P[4], prob=P[5], loss=P[6], ws=P[7], size=None):
+def balance(groups=2, tokens=50000, E=8, k=2, io=BF16, logits=P[0], mask=P[1], idx=P[2], w=P[3], counts=P[4], prob=P[5], loss=P[6], ws=P[7], size=None):
     lib = sw._load()
     size = lib.swimba_router_balance_workspace_bytes(groups, tokens, E) if size is None else size
     return lib.swimba_router_balance(groups, tokens, E, k, io, logits, mask, idx, w, counts, prob, loss, ws, size, None)
@@ -80,7 +80,7 @@ def test_router_bwd(kw, status):
     assert bwd(**kw) == status
 
 
-def linear(tokens=5, D=64, E=8, io=BF16, u=P[0], W=P[1], g=P[2], add=P[3], du=P[4], dW=P[5], ws=P[6], size=None):
+def linear(tokens=500, D=64, E=8, io=BF16, u=P[0], W=P[1], g=P[2], add=P[3], du=P[4], dW=P[5], ws=P[6], size=None):
     lib = sw._load()
     size = lib.swimba_router_linear_bwd_workspace_bytes(tokens, D, E) if size is None else size
     return lib.swimba_router_linear_bwd(tokens, D, E, io, u, W, g, add, du, dW, ws, size, None)
@@ -104,6 +104,13 @@ def test_workspaces_grow_with_the_call_and_end():
                     (lambda t: lib.swimba_router_linear_bwd_workspace_bytes(t, 768, 8), 1 << 25)):
         sizes = [f(t) for t in (0, 1, 100, 10000, 1 << 20, 1 << 30)]
         assert sizes == sorted(sizes) and 0 < sizes[0] and sizes[-1] <= most and all(s % 256 == 0 for s in sizes)
+    # 256 bytes: nothing is kept there, and no workspace is asked for (but the pointers behind it are)
+    assert lib.swimba_layer_norm_bwd_workspace_bytes(16, 768) == lib.swimba_router_balance_workspace_bytes(4, 150, 8) == 256
+    assert lib.swimba_router_linear_bwd_workspace_bytes(128, 768, 8) == 256
+    assert norm_bwd(tokens=16, D=768, ws=None, size=0, dx=None) == balance(groups=4, tokens=150, ws=None, size=0, loss=None) == NULL
+    assert linear(tokens=128, D=768, ws=None, size=0, W=None) == NULL
+    assert lib.swimba_router_balance_workspace_bytes(0, 1 << 20, 8) == 256    # no group: nothing to divide the slices among
+    assert lib.swimba_layer_norm_bwd_workspace_bytes(17, 768) == 5 * 2 * 768 * 4       # the sums of five blocks of four rows
     assert lib.swimba_layer_norm_bwd_workspace_bytes(-1, 768) == lib.swimba_layer_norm_bwd_workspace_bytes(1, 20000) == 0
     assert lib.swimba_router_balance_workspace_bytes(1, 1 << 31, 8) == lib.swimba_router_balance_workspace_bytes(1, 1, 257) == 0
     assert lib.swimba_router_linear_bwd_workspace_bytes(1, 0, 8) == lib.swimba_router_linear_bwd_workspace_bytes(1, 1 << 17, 8) == 0
