@@ -265,20 +265,26 @@ Shares shares_of(int64_t tokens, int64_t per_share, int64_t step, int64_t want)
     return {share, tokens > 0 ? (tokens + share - 1) / share : 0};
 }
 int experts_of(int E) { return E <= 16 ? 16 : E <= 32 ? 32 : 64; }                 // of a block of dW
-// Blocks that the chip holds at once at the kernels' registers, half of them for each product.
-int64_t blocks_of(int E) { return E <= 16 ? 384 : E <= 32 ? 512 : 256; }
+// Blocks that the chip holds at once at the kernels' registers, half of them for each product: two to a compute unit in fp32 and
+// for the sums of 64 experts, three below (16384 x 1024 x 16 bf16: 19.9 us with 384 blocks each, 22.0 with 512; 16384 x 768 x 8
+// fp32: 25.0 with 256, 28.3 with 384).  With 17 to 32 experts a few more are faster (16384 x 2048 x 32: 31.7 us with 512, 38.2
+// with 384), because shares come in whole steps.
+int64_t blocks_of(int E, int element) { return element == 4 || E > 32 ? 256 : E > 16 ? 512 : 384; }
 int64_t dw_per_share(int D, int E) { return (int64_t)((D + LB_COLS - 1) / LB_COLS) * ((E + experts_of(E) - 1) / experts_of(E)); }
-// (in steps of bf16 tokens, of which those of fp32 are half: the shares do not depend on the type)
-Shares dw_shares(int64_t tokens, int D, int E) { return shares_of(tokens, dw_per_share(D, E), dw_step<bf16>() * LB_WAVES, blocks_of(E)); }
+// (in steps of bf16 tokens, of which those of fp32 are half)
+Shares dw_shares(int64_t tokens, int D, int E, int element)
+{
+    return shares_of(tokens, dw_per_share(D, E), dw_step<bf16>() * LB_WAVES, blocks_of(E, element));
+}
 
 template <typename T>
 swimba_status linear_bwd(int64_t tokens, int D, int E, const void *u, const void *Wg, const void *dl, const void *du_add, void *du,
                          bool dW, float *part, hipStream_t st)
 {
-    const Shares sh = dw_shares(tokens, D, E);
+    const Shares sh = dw_shares(tokens, D, E, sizeof(T));
     auto go = [&](auto me, auto ks, auto nt) {
         const int64_t cols = (D + 16 * nt - 1) / (16 * nt);
-        const Shares us = shares_of(tokens, cols, 16 * LB_WAVES, blocks_of(E));
+        const Shares us = shares_of(tokens, cols, 16 * LB_WAVES, blocks_of(E, sizeof(T)));
         const unsigned wb = dW ? (unsigned)xcd_padded(dw_per_share(D, E) * sh.count) : 0;
         const unsigned ub = du ? (unsigned)(cols * us.count) : 0;
         if (wb + ub == 0) return;
@@ -310,16 +316,17 @@ swimba_status linear_bwd(int64_t tokens, int D, int E, const void *u, const void
 
 }  // namespace
 
+// (for bf16, which has as many shares as fp32 or more)
 size_t router_linear_bwd_bytes(int64_t tokens, int D, int E)
 {
-    const int64_t n = dw_shares(tokens, D, E).count;
+    const int64_t n = dw_shares(tokens, D, E, 2).count;
     return n > 1 ? (size_t)n * E * D * sizeof(float) : 0;
 }
 
 swimba_status launch_router_linear_bwd(int64_t tokens, int D, int E, int io_dtype, const void *u, const void *Wg, const void *dl,
                                        const void *du_add, void *du, float *dW, void *work, hipStream_t st)
 {
-    const int64_t shares = dw_shares(tokens, D, E).count;
+    const int64_t shares = dw_shares(tokens, D, E, io_dtype == SWIMBA_BF16 ? 2 : 4).count;
     // the sums of one share are dW itself
     float *const part = shares == 1 ? dW : (float *)work;
     if (tokens > 0) {
