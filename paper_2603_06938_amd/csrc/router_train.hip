@@ -209,7 +209,7 @@ template <typename T, int NP, int G, bool FULL>
 __global__ void __launch_bounds__(balance_most(NP, sizeof(T)))
 balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, int32_t *__restrict__ topk_idx,
                float *__restrict__ topk_w, float2 *__restrict__ part, int64_t tokens, int slices, int E, int K,
-               int32_t *__restrict__ counts, float *__restrict__ prob_mean, float *__restrict__ loss, int *__restrict__ ticket)
+               int32_t *__restrict__ counts, float *__restrict__ prob_mean, float *__restrict__ loss)
 {
     typedef Token<T, NP, G, FULL> Tok;
     __shared__ float psum[balance_most(NP, sizeof(T)) / 64][Tok::SIZE];
@@ -220,7 +220,6 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
     const int64_t stride = (int64_t)slices * (blockDim.x / G);
     const T *const z = logits + grp * tokens * E;
     if (threadIdx.x < Tok::SIZE) csum[threadIdx.x] = 0;
-    if (slices > 1 && threadIdx.x == 0 && blockIdx.x % slices == 0) ticket[grp] = 0;
     __syncthreads();
     float acc[NP][8] = {};
     struct Step {
@@ -332,69 +331,53 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
     else if (x < E) part[(int64_t)blockIdx.x * E + x] = make_float2(v, __int_as_float(c));
 }
 
-// The slices of a group joined, 64 experts to a block of 1024 threads: 16 waves take every 16th slice each.  Of several blocks
-// the one that is done last (a ticket that balance_kernel has set to zero) finishes the loss; what it adds up has an order of
-// its own, so that it does not matter which one that is.
-constexpr int LOSS_EXPERTS = 64;
+// The slices of a group joined by a block of 1024 threads: WIDTH threads side by side have PER experts each, the others every
+// (1024 / WIDTH)-th slice, 16 of them under way.
+template <int WIDTH, int PER>
 __global__ void __launch_bounds__(1024)
-balance_loss_kernel(const float2 *__restrict__ part, int slices, int E, int K, int32_t *counts, float *__restrict__ prob_mean,
-                    float *__restrict__ loss, float *psums, int *ticket)
+balance_loss_kernel(const float2 *__restrict__ part, int slices, int E, int K, int32_t *__restrict__ counts,
+                    float *__restrict__ prob_mean, float *__restrict__ loss)
 {
-    __shared__ float2 lds[16][LOSS_EXPERTS];
+    constexpr int ROWS = 1024 / WIDTH;
+    __shared__ float2 lds[ROWS][WIDTH * PER];
     __shared__ double fin[2][4];
-    __shared__ bool last;
-    const int blocks = (E + LOSS_EXPERTS - 1) / LOSS_EXPERTS;
-    const int64_t grp = blockIdx.x / blocks;
-    const int col = threadIdx.x % LOSS_EXPERTS, row = threadIdx.x / LOSS_EXPERTS, e = blockIdx.x % blocks * LOSS_EXPERTS + col;
-    int c = 0;
-    float p = 0.f;
-    if (e < E) {
+    const int64_t grp = blockIdx.x;
+    const int row = threadIdx.x / WIDTH, e = threadIdx.x % WIDTH * PER, n = E - e;
+    float p[PER] = {};
+    int c[PER] = {};
+    const float2 *const from = part + grp * slices * E + e;
+    if (n > 0) {
 #pragma unroll 16
-        for (int s = row; s < slices; s += 16) {
-            const float2 v = part[(grp * slices + s) * E + e];
-            p += v.x;
-            c += __float_as_int(v.y);
-        }
-    }
-    lds[row][col] = make_float2(p, __int_as_float(c));
-    __syncthreads();
-    p = 0.f;
-    c = 0;
-    if (row == 0) {
+        for (int s = row; s < slices; s += ROWS) {
+            Piece<float, 2 * PER> v;                           // the last expert of an odd number stands alone
+            v.template load<PER == 2>((const float *)(from + (int64_t)s * E), 2 * n);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            p += lds[i][col].x;
-            c += __float_as_int(lds[i][col].y);
+            for (int i = 0; i < PER; ++i) { p[i] += v.get(2 * i); c[i] += (int)v.v[2 * i + 1]; }
         }
     }
-    if (blocks > 1) {
-        if (row == 0 && e < E) {
-            __hip_atomic_store(psums + grp * E + e, p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(counts + grp * E + e, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) last = __hip_atomic_fetch_add(ticket + grp, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
-        __syncthreads();
-        if (!last) return;
-        __threadfence();
-        const int x = threadIdx.x;
-        if (x < E) {
-            p = __hip_atomic_load(psums + grp * E + x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            c = __hip_atomic_load(counts + grp * E + x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) lds[row][e + i] = make_float2(p[i], __int_as_float(c[i]));
+    __syncthreads();
+    float sum = 0.f;
+    int count = 0;
+    if (threadIdx.x < WIDTH * PER) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            sum += lds[i][threadIdx.x].x;
+            count += __float_as_int(lds[i][threadIdx.x].y);
         }
     }
-    balance_finish(p, c, grp, E, K, counts, prob_mean, loss, fin);
+    balance_finish(sum, count, grp, E, K, counts, prob_mean, loss, fin);
 }
 
 namespace {
 
-int power_of_two(int n)
+int lanes_of(int E)                                            // of a token, eight experts to a lane
 {
-    int p = 1;
-    while (p < n) p *= 2;
-    return p;
+    int n = 1;
+    while (8 * n < E) n *= 2;
+    return n;
 }
-int lanes_of(int E) { return power_of_two((E + 7) / 8); }      // of a token, eight experts to a lane
 // Eight lanes at most for the routing: steps over lanes cost as much as three experts of a lane, and with few tokens to a wave
 // so does what is done once for all of them.
 constexpr int pieces_for(int lanes) { return lanes <= 4 ? 1 : lanes <= 8 ? 2 : 4; }
@@ -402,8 +385,8 @@ int pieces_of(int E) { return pieces_for(lanes_of(E)); }
 int routing_lanes_of(int E) { return lanes_of(E) / pieces_of(E); }
 
 // Threads of a block and slices of a group.  A group that a block walks in four steps or less stays with one block, without a
-// second launch; beyond, a slice is a step or more, and the slices of all groups are some 256 (a few more where groups are
-// many), which fill the chip with waves and are soon added up.
+// second launch; beyond, a slice is a step or more, and the slices of all groups are no more than the compute units: a block of
+// 1024 threads fills one, and a 257th would run by itself (131072 x 256: 53.0 us with 257, 35.6 with 256).
 struct Slices { int threads; int64_t count; };
 Slices balance_slices(int64_t groups, int64_t tokens, int E, int element)
 {
@@ -414,7 +397,7 @@ Slices balance_slices(int64_t groups, int64_t tokens, int E, int element)
         while (n < most && n < threads) n *= 2;
         return {n, 1};
     }
-    const int64_t slices = 1024 / most * 256 / groups + 1;
+    const int64_t slices = 256 / groups;
     return {most, steps < slices ? steps : slices};
 }
 
@@ -440,12 +423,11 @@ void with_lanes(int E, F &&f)
 
 }  // namespace
 
-// scratch of the sums in slices: part, then the joined sums of the probabilities and a ticket for each group
-// (for the type that takes more slices)
 size_t balance_bytes(int64_t groups, int64_t tokens, int E)
 {
+    // (for the type that takes more slices)
     const int64_t a = balance_slices(groups, tokens, E, 2).count, b = balance_slices(groups, tokens, E, 4).count, n = a > b ? a : b;
-    return n > 1 ? (size_t)groups * (n * E * sizeof(float2) + E * sizeof(float) + sizeof(int)) : 0;
+    return n > 1 ? (size_t)groups * n * E * sizeof(float2) : 0;
 }
 
 swimba_status launch_router_balance(int64_t groups, int64_t tokens, int E, int K, int io_dtype, const void *logits,
@@ -455,21 +437,19 @@ swimba_status launch_router_balance(int64_t groups, int64_t tokens, int E, int K
     if (groups == 0) return SWIMBA_OK;
     const Slices s = balance_slices(groups, tokens, E, io_dtype == SWIMBA_BF16 ? 2 : 4);
     float2 *const part = (float2 *)work;
-    float *const psums = (float *)(part + groups * s.count * E);
-    int *const ticket = (int *)(psums + groups * E);
     with_lanes(E, [&](auto lanes, auto, auto full) {
         constexpr int NP = pieces_for(lanes()), G = lanes() / NP;
         auto go = [&](auto kernel, auto *z) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)(groups * s.count)), dim3(s.threads), 0, st, z, mask, topk_idx, topk_w, part, tokens,
-                               (int)s.count, E, K, counts, prob_mean, loss, ticket);
+                               (int)s.count, E, K, counts, prob_mean, loss);
         };
         if (io_dtype == SWIMBA_BF16) go(balance_kernel<bf16, NP, G, full()>, (const bf16 *)logits);
         else go(balance_kernel<float, NP, G, full()>, (const float *)logits);
     });
     SWIMBA_CHECK_LAUNCH();
     if (s.count > 1) {
-        hipLaunchKernelGGL(balance_loss_kernel, dim3((unsigned)(groups * ((E + LOSS_EXPERTS - 1) / LOSS_EXPERTS))), dim3(1024), 0, st, part, (int)s.count, E, K,
-                           counts, prob_mean, loss, psums, ticket);
+        const auto kernel = E <= 64 ? balance_loss_kernel<64, 1> : balance_loss_kernel<128, 2>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(1024), 0, st, part, (int)s.count, E, K, counts, prob_mean, loss);
         SWIMBA_CHECK_LAUNCH();
     }
     return SWIMBA_OK;
