@@ -2,8 +2,11 @@
 //   balance   pi = softmax(logits), K = top-k;  counts[e] = #{t : e in K_t}, P[e] = mean_t pi_t[e],  loss = E sum_e f_e P_e with
 //             f_e = counts[e] / (k n), over the n tokens of a group that count
 //   logits    g_t[e] = [e in K_t] dw + d_loss (E / n) f_e,   d_logits = pi (g - <pi, g>)
-// A token lies in G lanes, eight consecutive experts to a lane: one 16-byte piece of a bf16 row, so that a wave's loads are
-// contiguous where the experts fill the lanes.
+// A token lies in G lanes, in pieces of eight consecutive experts: 16 bytes of a bf16 row, so that a wave's loads are contiguous
+// where the experts fill the lanes.
+// Few experts are bound by memory and by their launches (2 x 16384 x 16 with padding 11.4 us, its gradient 4.9); many by what
+// the vector units have to issue: of the 30 us of 131072 x 256 top-8 in bf16 (75 MB, 12 us at the rate of a copy) they are busy
+// nine tenths, half of it with the picks.  The gradient is bound by memory (65536 x 256 fp32 31 us, 4.5 TB/s).
 #include "rows.hpp"
 
 namespace swimba {
@@ -273,20 +276,22 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
                 for (int j = 0; j < 8; ++j) other |= tok.real(i, j) && s.p[i].get(j) != -INFINITY;
             on = on && over_group<G>(other, umax);
         }
-        // exp(f - m) as exp2(f c - m c) in one rounding; m c, and with it the weights, would overflow for the largest of numbers
+        // exp(f - m) as exp2(f c - m c) in one rounding, with m c as it is rounded: the weights and their sum have the same factor
+        // then, which is 1.01 at most up to |m| = 10^5.  Beyond, the difference is taken first: by each token for itself, so that
+        // nothing depends on the tokens beside it.
         float p[NP][8], Z = 0.f;
         const float mc = m * LOG2E;
-        const bool far = __any(fabsf(m) > 2e38f);
+        const bool far = !(fabsf(m) <= 1e5f);
 #pragma unroll
         for (int i = 0; i < NP; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 p[i][j] = tok.real(i, j) ? fast_exp2(fmaf(s.p[i].get(j), LOG2E, -mc)) : 0.f;
-        if (far) {
+        if (__any(far)) {
 #pragma unroll
             for (int i = 0; i < NP; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) p[i][j] = tok.real(i, j) ? route_exp(s.p[i].get(j) - m) : 0.f;
+                for (int j = 0; j < 8; ++j) p[i][j] = !tok.real(i, j) ? 0.f : far ? route_exp(s.p[i].get(j) - m) : p[i][j];
         }
 #pragma unroll
         for (int i = 0; i < NP; ++i)
@@ -296,7 +301,7 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
         if (t + at < tokens) {
             auto put = [&](int r, int x, float f) __attribute__((always_inline)) {
                 if (topk_idx) topk_idx[row * K + r] = x;
-                if (topk_w) topk_w[row * K + r] = route_exp(f - m) * invZ;
+                if (topk_w) topk_w[row * K + r] = (far ? route_exp(f - m) : fast_exp2(fmaf(f, LOG2E, -mc))) * invZ;
                 if (on) atomicAdd(&csum[x], 1);                // whole numbers: the order does not matter
             };
 #pragma unroll

@@ -174,7 +174,4 @@ __device__ __forceinline__ void sum_over(float (&v)[N], int &first, int lane)
     }
 }
 
-// sum over the 64 lanes, in every lane
-__device__ __forceinline__ float wave_sum(float v) { return group_sum<64>(v); }
-
 }  // namespace swimba

@@ -8,8 +8,8 @@ from train_ref import IO, half, norm, norm_bwd, within
 pytestmark = pytest.mark.gpu
 
 # both sides of every width at which another number of lanes or waves takes a row, and rows that start at any element
-WIDTHS = [1, 2, 7, 8, 9, 63, 64, 257, 504, 511, 512, 513, 768, 1001, 1024, 1025, 2047, 2048, 2056, 4096, 4099, 8192, 8200,
-          12345, 16384]
+WIDTHS = [1, 2, 7, 8, 9, 16, 63, 64, 65, 100, 127, 128, 129, 256, 257, 504, 511, 512, 513, 768, 1001, 1024, 1025, 2047,
+          2048, 2056, 4096, 4099, 8192, 8200, 12345, 16384]
 TYPES = [("f32", None), ("bf16", None), ("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")]
 
 
@@ -75,7 +75,8 @@ def test_backward(D, io, res):
     assert (behind == 7).all()
 
 
-@pytest.mark.parametrize("T,D", [(1, 768), (2, 8), (3, 513), (64, 768), (65, 1000), (511, 64), (2049, 24), (3000, 130), (700, 2048), (600, 9000)])
+@pytest.mark.parametrize("T,D", [(1, 768), (2, 8), (3, 513), (64, 768), (65, 1000), (511, 64), (2049, 24), (3000, 130),
+                                 (301, 64), (777, 100), (4097, 128), (700, 2048), (600, 9000)])
 @pytest.mark.parametrize("io,res", [("bf16", "f32"), ("f32", None)])
 def test_numbers_of_rows(T, D, io, res):
     x, residual, gamma, beta = case(T, D, io, res, T)

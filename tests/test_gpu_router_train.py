@@ -94,6 +94,27 @@ def test_masked_logits(E, k, io):
     assert (got[:, 3::11] == 0).all()
 
 
+@pytest.mark.parametrize("E,k", [(1, 1), (8, 2), (20, 3), (64, 8), (128, 4), (256, 8)])
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_logits_far_from_zero(E, k, io):
+    """The weights depend on differences alone, however far from zero the logits are: one size to a token, from 10 to the
+    largest of the type, both signs, tokens of all sizes side by side in a wave."""
+    L = 320
+    gen = torch.Generator().manual_seed(E)
+    size = 10.0 ** (torch.arange(L) % 39).double()
+    size = torch.minimum(size, torch.tensor(3e38, dtype=torch.float64)) * torch.where(torch.arange(L) % 2 == 0, 1.0, -1.0)
+    steps = torch.randint(0, 12, (L, E), generator=gen)
+    z = (size[:, None] * torch.ones(E)).to(IO[io])
+    ulp = (torch.nextafter(z.abs(), torch.tensor(float("inf"), dtype=z.dtype)) - z.abs()).double()
+    z = (z.double() + torch.where(ulp < 1, steps * 0.25, steps * ulp * (ulp < 1e36))).to(IO[io])[None].to("cuda:0")
+    assert z.isfinite().all()
+    out = sw.swimba_router_balance(z, k)
+    check_balance(z, k, None, False, out)
+    one = torch.ones(1, device="cuda:0")
+    ref, bound = routing_bwd(z, out.topk_idx, out.topk_w, out.counts, one)
+    within(sw.swimba_router_bwd(z, out.topk_idx, out.topk_w, out.counts, one), ref, bound + half(z.dtype) * (ref.abs() + bound), "d_logits")
+
+
 @pytest.mark.parametrize("E,k", EXPERTS)
 def test_logits_that_differ_in_their_last_bits(E, k):
     """fp32 logits in runs that differ by a few of their lowest bits, and equal ones among them: pairs, runs across the last
