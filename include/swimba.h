@@ -448,13 +448,11 @@ swimba_status swimba_layer_norm_bwd(int64_t tokens, int32_t d_model, int32_t io_
  *   logits   (groups, tokens, E) io [in]
  *   mask     (groups, tokens) uint8 [in]  0: the token does not count (padding); NULL: all count.  Its logits reach
  *            nothing but its own topk_idx and topk_w, whatever they hold.  A token whose logits are all -inf does not count either.
- *   topk_idx, topk_w (groups, tokens, k) [out]  of every token: the experts of swimba_router_topk and, to the rounding of the sum
- *            over the experts, its weights;
- *            NULL = not wanted
+ *   topk_idx, topk_w (groups, tokens, k) [out]  of every token: the experts of swimba_router_topk and, to the rounding of
+ *            the sum over the experts, its weights; NULL = not wanted
  *   counts   (groups, E) int32 [out]    prob_mean (groups, E) fp32 [out]  NULL = not wanted    loss (groups) fp32 [out]
  * A logit that is NaN or +inf in a token that counts makes the probabilities and the loss of its group NaN.
- * At most 2^31 - 1 tokens to a group and 2^38 in all.  Element-aligned pointers; rows of logits that start 16-byte
- * aligned (by pointer and E) are read in larger pieces.
+ * At most 2^20 groups, 2^31 - 1 tokens to a group and 2^38 in all.  Element-aligned pointers, rows of any width.
  *   workspace >= swimba_router_balance_workspace_bytes(groups, tokens, nexperts), 256-byte aligned.
  *            Where that is 256, its smallest, nothing is kept there and it may be NULL.
  */
@@ -489,8 +487,8 @@ swimba_status swimba_router_bwd(int64_t groups, int64_t tokens, int32_t nexperts
  *   du       (tokens, d_model) io [out]  NULL = not wanted; may be the buffer of du_add
  *   dW_g     (E, d_model) fp32 [out]     NULL = not wanted
  * fp32 accumulation; du is rounded once, dW_g is not rounded, its sum over the tokens is taken in an order that sizes alone decide.
- * u is read for dW_g only, W_g for du only; the other may be NULL.  Limits, alignment (du, du_add as u) and the
- * element-wise reading of rows that are no multiple of 16 bytes as in swimba_router_linear; dW_g by element.
+ * u is read for dW_g only, W_g for du only; the other may be NULL.  Limits and alignment (du, du_add as u) as in
+ * swimba_router_linear, rows of any width; dW_g by element.
  *   workspace >= swimba_router_linear_bwd_workspace_bytes(tokens, d_model, nexperts), 256-byte aligned.
  *            Where that is 256, its smallest, nothing is kept there and it may be NULL.
  */
