@@ -38,7 +38,7 @@ __device__ __forceinline__ uint32_t umin(uint32_t a, uint32_t b) { return a < b 
 // One token in G lanes, 8 NP experts to a lane: piece i of lane l are the experts from 8 (l + G i) on.
 // A key is smaller the earlier its expert is picked.  Its lowest bits are the expert's number, so that all keys differ and
 // name their experts; above them lies the place of a bf16 logit, or the upper 24 bits of an fp32 one's, which do not decide
-// between logits that agree that far: those are picked by the whole of them (`close`).  The lane's part of the number, 8 l,
+// between logits that agree that far: those are put in order by the whole of them (`close`).  The lane's part of the number, 8 l,
 // is not in the stored keys: it is added to what a lane has found.  FULL: the experts fill the lanes.
 template <typename T, int NP, int G, bool FULL> struct Token {
     static constexpr bool BF = sizeof(T) == 2;
@@ -120,7 +120,7 @@ template <typename T, int NP, int G, bool FULL> struct Token {
             v[i] = BF ? at_place(mine >> 16) : 0.f;
         }
         if constexpr (!BF) {
-            // agreement that goes on behind that pick leaves the choice to exact()
+            // agreement that goes on behind that pick leaves the choice to settle()
             if (__any(end) && end && behind >= 0) {
                 const uint32_t n = next(b);
                 if (n > b && near(b, n)) behind = -2;
@@ -128,26 +128,27 @@ template <typename T, int NP, int G, bool FULL> struct Token {
         }
         return close;
     }
-    // the same by whole places, equal ones by the expert
-    __device__ __forceinline__ void exact(int K, int (&e)[SLOTS]) const
+    // Which of the logits that agree with the last pick in their keys' upper bits are picked, where more do than there are picks left
+    // (`open`): by the lower bits of their places, equal ones by the expert.  The picks with other upper bits stay.
+    __device__ __forceinline__ void settle(int K, int (&e)[SLOTS], const float (&v)[SLOTS], bool open) const
     {
-        uint32_t last = 0;
-        int x = -1;
-        auto place = [&](int i, int j) { return place_of(p[i].get(j)); };
+        uint32_t upper = 0, before = 0;
 #pragma unroll
-        for (int i = 0; i < SLOTS; ++i) {
-            const int rounds = min(K - i * G, G);
-#pragma unroll 1
-            for (int r = 0; r < rounds; ++r) {
-                auto after = [&](int q, int j) {
-                    const uint32_t o = place(q, j);
-                    return real(q, j) && (o > last || (o == last && expert(q, j) > x));
-                };
-                const uint32_t o = over([&](int q, int j) { return after(q, j) ? place(q, j) : NONE; }, umin);
-                x = (int)over([&](int q, int j) { return after(q, j) && place(q, j) == o ? (uint32_t)expert(q, j) : 1u << 20; }, umin);
-                last = o;
-                e[i] = l == r ? x : e[i];
-            }
+        for (int i = 0; i < SLOTS; ++i) upper = i * G + l < K ? umax(upper, place_of(v[i]) & ~LOW) : upper;
+        upper = over_group<G>(upper, umax);
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) before += i * G + l < K && place_of(v[i]) < upper;
+        int r = open ? (int)over_group<G>(before, add_u32) : K;
+        uint32_t from = 0;
+        while (__any(r < K)) {
+            const uint32_t n = over([&](int i, int j) {
+                const uint32_t o = place_of(p[i].get(j)) - upper, k = o << 8 | expert(i, j);
+                return o <= LOW && real(i, j) && k >= from ? k : NONE;
+            }, umin);
+#pragma unroll
+            for (int i = 0; i < SLOTS; ++i) e[i] = r < K && i * G + l == r ? (int)(n & LOW) : e[i];
+            from = n + 1;
+            ++r;
         }
     }
     // Where the picks that lie in the lanes, and the one behind them, stand among themselves by whole places: rank[i] of the lane's
@@ -253,16 +254,23 @@ balance_kernel(const T *__restrict__ logits, const uint8_t *__restrict__ mask, i
         const int64_t row = grp * tokens + (t + at < tokens ? t + at : tokens - 1);
         int e[Tok::SLOTS], rank[Tok::SLOTS], behind = -1, rank_b = K;
         float v[Tok::SLOTS];
-        const bool close = tok.picks(K, e, v, behind);
-        if (!Tok::BF && __any(behind == -2)) {
-            tok.exact(K, e);
-            behind = -1;
+        bool close = tok.picks(K, e, v, behind);
+        if constexpr (!Tok::BF) {                              // the keys do not hold the whole of the logits
+            auto take = [&] {
+#pragma unroll
+                for (int i = 0; i < Tok::SLOTS; ++i)
+                    if (i * G + l < K) v[i] = to_float(logits[row * E + e[i]]);
+            };
+            take();
+            close = close && t + at < tokens;                  // (behind the last token all logits are zero)
+            if (__any(close && behind == -2)) {
+                tok.settle(K, e, v, close && behind == -2);
+                take();
+            }
+            if (behind == -2) behind = -1;
         }
 #pragma unroll
-        for (int i = 0; i < Tok::SLOTS; ++i) {
-            rank[i] = i * G + l;
-            if (!Tok::BF && rank[i] < K) v[i] = to_float(logits[row * E + e[i]]);      // its key does not hold the whole of it
-        }
+        for (int i = 0; i < Tok::SLOTS; ++i) rank[i] = i * G + l;
         if constexpr (!Tok::BF) {
             if (__any(close)) rank_b = tok.rank_of(K, e, v, behind, to_float(logits[row * E + (behind >= 0 ? behind : 0)]), rank);
         }
@@ -389,21 +397,25 @@ constexpr int pieces_for(int lanes) { return lanes <= 4 ? 1 : lanes <= 8 ? 2 : 4
 int pieces_of(int E) { return pieces_for(lanes_of(E)); }
 int routing_lanes_of(int E) { return lanes_of(E) / pieces_of(E); }
 
-// Threads of a block and slices of a group.  A group that a block walks in four steps or less stays with one block, without a
-// second launch; beyond, a slice is a step or more, and the slices of all groups are no more than the compute units: a block of
-// 1024 threads fills one, and a 257th would run by itself (131072 x 256: 53.0 us with 257, 35.6 with 256).
+// Threads of a block and slices of a group.  A group that a block walks in one step, or in two with eight experts to a lane, stays
+// with it, without a second launch (8.7 us with 171 tokens of 256 experts top-8 in a step; with 512 in four steps 26.3, in two
+// launches 13).  Beyond, a slice is a step or more, and the slices of all groups are no more than the compute units: a block of
+// 1024 threads fills one, and a 257th would run by itself (131072 x 256: 53.0 us with 257, 35.6 with 256).  Smaller blocks where
+// they are enough for that.
 struct Slices { int threads; int64_t count; };
+int64_t routing_threads(int64_t tokens, int E) { return tokens * routing_lanes_of(E); }
+bool one_block(int64_t groups, int64_t tokens, int E, int element)
+{
+    return groups > 128 || groups == 0 || routing_threads(tokens, E) <= balance_most(pieces_of(E), element) * (pieces_of(E) == 1 ? 2 : 1);
+}
 Slices balance_slices(int64_t groups, int64_t tokens, int E, int element)
 {
     const int most = balance_most(pieces_of(E), element);
-    const int64_t threads = tokens * routing_lanes_of(E), steps = (threads + most - 1) / most;
-    if (steps <= 4 || groups >= 256 || groups == 0) {
-        int n = 256;
-        while (n < most && n < threads) n *= 2;
-        return {n, 1};
-    }
-    const int64_t slices = 256 / groups;
-    return {most, steps < slices ? steps : slices};
+    const int64_t threads = routing_threads(tokens, E), slices = one_block(groups, tokens, E, element) ? 1 : 256 / groups;
+    int n = 256;
+    while (n < most && (threads + n - 1) / n > slices) n *= 2;
+    const int64_t steps = (threads + n - 1) / n;
+    return {n, slices == 1 || steps < 2 ? 1 : steps < slices ? steps : slices};
 }
 
 // f(lanes, whether the last piece is short, whether the experts fill the lanes) as constants
@@ -430,9 +442,10 @@ void with_lanes(int E, F &&f)
 
 size_t balance_bytes(int64_t groups, int64_t tokens, int E)
 {
-    // (for the type that takes more slices)
-    const int64_t a = balance_slices(groups, tokens, E, 2).count, b = balance_slices(groups, tokens, E, 4).count, n = a > b ? a : b;
-    return n > 1 ? (size_t)groups * n * E * sizeof(float2) : 0;
+    // for either type, and for fewer tokens as well
+    if (one_block(groups, tokens, E, 2) && one_block(groups, tokens, E, 4)) return 0;
+    const int64_t n = groups * ((routing_threads(tokens, E) + 255) / 256);
+    return (size_t)(n < 256 ? n : 256) * E * sizeof(float2);
 }
 
 swimba_status launch_router_balance(int64_t groups, int64_t tokens, int E, int K, int io_dtype, const void *logits,
