@@ -6,6 +6,8 @@
 //   dW  k runs over the tokens: the wave keeps its sums (16 experts a tile) while it walks its tokens; the sums of a block's
 //       waves are joined in LDS, those of the blocks by a second launch
 //   du  k runs over the experts: W is kept in registers, 16 tokens at a time
+// 16384 x 768 x 8 bf16 with both products (51 MB) 14.5 us, 4.1 of them the second launch; 32768 x 2048 x 64 with du_add (407 MB)
+// 95.8 us, 4.25 TB/s; 16384 x 2048 x 256 82.7 us, 415 TFLOP/s; 16384 x 2048 x 128 fp32 175 us, 98 of 154 TFLOP/s.
 #include "rows.hpp"
 
 namespace swimba {
@@ -29,9 +31,10 @@ __device__ __forceinline__ f32x4_t mfma4(uint32_t a, uint32_t b, f32x4_t c)
 template <typename T> constexpr int dw_step() { return sizeof(T) == 2 ? 32 : 16; }
 constexpr int LB_COLS = 128;           // features of a wave
 constexpr int LB_WAVES = 4;
+typedef f32x4_t Join[4][2][64];       // a tile of a wave: rows 4 kg + v, halves of a lane's eight columns
 
 // Where the last pieces of a row would pass its end (columns of u and du, experts of dl), they are moved to end with it: the
-// lane then works on some columns that its neighbour has as well, and stores only what is past `own`.
+// lane then has some elements that its neighbour has as well, and stores, or takes into a sum, only those from `own` on.
 struct Cols {
     int at, own;                       // first element of the lane's piece, and of those that are its own
     __device__ __forceinline__ Cols(int first, int size, int W) : at(size >= W ? min(first, size - W) : first), own(first) {}
@@ -41,7 +44,7 @@ struct Cols {
 // A step is 32 tokens, 8 kg .. 8 kg + 7 in a lane, in bf16 (one instruction), and 16, kg + 4 j, in fp32 (four).
 template <typename T, int ME>
 __device__ __forceinline__ void dw_block(const T *__restrict__ u, const T *__restrict__ dl, float *__restrict__ part,
-                                         float (*lds)[LB_COLS + 4], int64_t tokens, int D, int E, int col, int eb, int64_t split,
+                                         Join *lds, int64_t tokens, int D, int E, int col, int eb, int64_t split,
                                          int64_t share)
 {
     constexpr bool BF = sizeof(T) == 2;
@@ -117,26 +120,37 @@ __device__ __forceinline__ void dw_block(const T *__restrict__ u, const T *__res
                     for (int j = 0; j < ME; ++j) acc[j][i] = mfma4(s.g[r][j], s.u[r].v[i], acc[j][i]);
         }
     }
-    // lds[e][column], counted from the block's first
-    for (int w = 0; w < LB_WAVES; ++w) {
-        if (wave == w) {
+    // A tile's rows 4 kg + v of the four waves are joined by wave v, in the order of the waves.
+    const int m = 4 * kg + wave;
+    const Cols ce(eb * 16 * ME + ME * m, E, ME);
 #pragma unroll
-            for (int j = 0; j < ME; ++j)
+    for (int j = 0; j < ME; ++j) {
+        if (j) __syncthreads();
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    float *row = &lds[ME * (4 * kg + v) + j][8 * n];
+        for (int v = 0; v < 4; ++v)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) row[i] = w ? row[i] + acc[j][i][v] : acc[j][i][v];
-                }
-        }
+            for (int h = 0; h < 2; ++h)
+                lds[wave][v][h][lane] = f32x4_t{acc[j][4 * h][v], acc[j][4 * h + 1][v], acc[j][4 * h + 2][v], acc[j][4 * h + 3][v]};
         __syncthreads();
-    }
-    for (int i = threadIdx.x; i < 16 * ME * LB_COLS; i += 64 * LB_WAVES) {
-        const int r = i / LB_COLS, q = i % LB_COLS;
-        // row r and column q of the tiles are expert and feature
-        const Cols ce(eb * 16 * ME + r / ME * ME, E, ME), cd(col * LB_COLS + q / 8 * 8, D, 8);
-        const int e = ce.at + r % ME, d = cd.at + q % 8;
-        if (e >= ce.own && e < E && d >= cd.own && d < D) part[(split * E + e) * D + d] = lds[r][q];
+        f32x4_t sum[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            sum[h] = lds[0][wave][h][lane];
+#pragma unroll
+            for (int w = 1; w < LB_WAVES; ++w) sum[h] += lds[w][wave][h][lane];
+        }
+        const int e = ce.at + j;
+        if (e < ce.own || e >= E) continue;
+        float *const to = part + (split * E + e) * D + c.at;
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = sum[i / 4][i % 4];
+        if (c.at == c.own) store_piece<true>(to, f, D - c.at);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i >= c.own - c.at) to[i] = f[i];
+        }
     }
 }
 
@@ -151,7 +165,7 @@ __device__ __forceinline__ void du_block(const T *__restrict__ Wg, const T *__re
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, kg = lane >> 4;
     const int64_t t0 = split * share, t1 = min(t0 + share, tokens);
     const Cols c(col * 16 * NT + NT * n, D, NT);
-    const int width = D >= NT ? (c.own < D ? NT : 0) : D - c.at;       // elements of the lane's piece that exist
+    const int width = D >= NT ? (c.own < D ? NT : 0) : D - c.at;       // elements of the lane's piece that exist and count
     struct Step {
         Piece<T, R> a[KS];
         Piece<T, NT> add[4];
@@ -160,10 +174,13 @@ __device__ __forceinline__ void du_block(const T *__restrict__ Wg, const T *__re
         const T *g = dl + t * E, *add = du_add + t * D;
         const int left = (int)min((int64_t)16, t1 - t);
         const uint32_t row = min(n, left - 1) * E;
+        int first = R * kg;
+        asm volatile("" : "+v"(first));                        // the places of all steps, kept, would take the registers
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            const int e = 4 * R * k + R * kg;
-            s.a[k].template load<true>(g + row + e, E - e);
+            const Cols x(4 * R * k + first, E, R);
+            if (E < R) s.a[k].template load<true>(g + row + x.at, E - x.at);
+            else s.a[k].template load<false>(g + row + x.at, R);
         }
         if (du_add) {
 #pragma unroll
@@ -178,10 +195,18 @@ __device__ __forceinline__ void du_block(const T *__restrict__ Wg, const T *__re
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
         Piece<T, NT> p[R];
+        const Cols x(R * (4 * k + kg), E, R);
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int e = 4 * R * k + R * kg + j;
-            p[j].template load<true>(Wg + (uint32_t)(e * D + c.at), e < E ? width : 0);
+            const T *const row = Wg + (uint32_t)((x.at + j) * D + c.at);
+            if (E >= R && D >= NT) p[j].template load<false>(row, NT);
+            else p[j].template load<true>(row, x.at + j < E ? width : 0);
+        }
+        if (4 * R * (k + 1) > E) {
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+#pragma unroll
+                for (uint32_t &q : p[j].v) q = x.at + j < x.own ? 0 : q;
         }
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -199,8 +224,12 @@ __device__ __forceinline__ void du_block(const T *__restrict__ Wg, const T *__re
         } else
             fetch(s, t);
         f32x4_t acc[NT] = {};
+        int first = R * kg;
+        asm volatile("" : "+v"(first));
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+        for (int k = 0; k < KS; ++k) {
+            const Cols x(4 * R * k + first, E, R);
+            if (4 * R * (k + 1) > E) s.a[k].drop(x.own - x.at);
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
                 if constexpr (BF) acc[i] = mfma16(s.a[k].v, w[k][i], acc[i]);
@@ -209,6 +238,7 @@ __device__ __forceinline__ void du_block(const T *__restrict__ Wg, const T *__re
                     for (int q = 0; q < 4; ++q) acc[i] = mfma4(s.a[k].v[q], w[k][i][q], acc[i]);
                 }
             }
+        }
         T *const out = du + t * D;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
@@ -236,7 +266,7 @@ __global__ void __launch_bounds__(64 * LB_WAVES) __attribute__((amdgpu_waves_per
 linear_bwd_kernel(const T *__restrict__ u, const T *__restrict__ Wg, const T *__restrict__ dl, const T *du_add, T *du,
                   float *__restrict__ part, int64_t tokens, int D, int E, unsigned wblocks, Shares ws, Shares us)
 {
-    __shared__ float lds[16 * ME][LB_COLS + 4];
+    __shared__ Join lds[LB_WAVES];
     if (blockIdx.x < wblocks) {
         // the blocks of one share and its columns, which read the same u, follow each other on one XCD
         const int cols = (D + LB_COLS - 1) / LB_COLS, eblocks = (E + 16 * ME - 1) / (16 * ME);
@@ -265,10 +295,11 @@ Shares shares_of(int64_t tokens, int64_t per_share, int64_t step, int64_t want)
     return {share, tokens > 0 ? (tokens + share - 1) / share : 0};
 }
 int experts_of(int E) { return E <= 16 ? 16 : E <= 32 ? 32 : 64; }                 // of a block of dW
-// Blocks that the chip holds at once at the kernels' registers, half of them for each product: two to a compute unit in fp32 and
-// for the sums of 64 experts, three below (16384 x 1024 x 16 bf16: 19.9 us with 384 blocks each, 22.0 with 512; 16384 x 768 x 8
-// fp32: 25.0 with 256, 28.3 with 384).  With 17 to 32 experts a few more are faster (16384 x 2048 x 32: 31.7 us with 512, 38.2
-// with 384), because shares come in whole steps.
+// Blocks that sum dW, half of those that the chip holds at once at the kernels' registers: of two to a compute unit in fp32 and
+// for the sums of 64 experts, of three below (16384 x 1024 x 16 bf16: 17.3 us with 384 blocks, 18.6 with 512; 16384 x 768 x 8
+// fp32: 22.2 with 256, 24.3 with 384).  With 17 to 32 experts a few more are faster (16384 x 2048 x 32: 29.5 us with 512, 33.8
+// with 384), because shares come in whole steps.  du has three times as many, which start as others end, so that both streams of
+// memory run to the end (16384 x 2048 x 16: 30.1 us, 34.6 with as many as dW has; x 64 35.1 and 41.5).
 int64_t blocks_of(int E, int element) { return element == 4 || E > 32 ? 256 : E > 16 ? 512 : 384; }
 int64_t dw_per_share(int D, int E) { return (int64_t)((D + LB_COLS - 1) / LB_COLS) * ((E + experts_of(E) - 1) / experts_of(E)); }
 // (in steps of bf16 tokens, of which those of fp32 are half)
@@ -284,7 +315,7 @@ swimba_status linear_bwd(int64_t tokens, int D, int E, const void *u, const void
     const Shares sh = dw_shares(tokens, D, E, sizeof(T));
     auto go = [&](auto me, auto ks, auto nt) {
         const int64_t cols = (D + 16 * nt - 1) / (16 * nt);
-        const Shares us = shares_of(tokens, cols, 16 * LB_WAVES, blocks_of(E, sizeof(T)));
+        const Shares us = shares_of(tokens, cols, 16 * LB_WAVES, 3 * blocks_of(E, sizeof(T)));
         const unsigned wb = dW ? (unsigned)xcd_padded(dw_per_share(D, E) * sh.count) : 0;
         const unsigned ub = du ? (unsigned)(cols * us.count) : 0;
         if (wb + ub == 0) return;

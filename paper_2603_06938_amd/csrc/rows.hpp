@@ -48,6 +48,14 @@ template <typename T, int W> struct Piece {
                 }
         }
     }
+    __device__ __forceinline__ void drop(int n)                // the first n become zero
+    {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            if constexpr (sizeof(T) == 4) v[i] = i < n ? 0 : v[i];
+            else v[i] = 2 * i + 1 < n ? 0 : 2 * i < n ? v[i] & 0xffff0000u : v[i];
+        }
+    }
     __device__ __forceinline__ float get(int i) const
     {
         if constexpr (sizeof(T) == 4) return __uint_as_float(v[i]);

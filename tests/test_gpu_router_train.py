@@ -335,6 +335,30 @@ def test_linear_backward_parts():
     assert none.du.shape == (0, 200) and (none.dW_g == 0).all()
 
 
+@pytest.mark.parametrize("E", [1, 3, 5, 8, 9, 20, 30, 61, 70, 100, 127, 130, 190, 255])
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_linear_backward_infinities(E, io):
+    """An infinite gradient of one logit, or weight of one feature, reaches what the formula says and as it says: with experts
+    that end inside a piece no other expert's factor turns it into NaN."""
+    T, D = 90, 77
+    u, W, g, _ = linear_case(T, D, E, io, E)
+    want = sw.swimba_router_linear_bwd(u, W, g)
+    for t, e, c in ((0, 0, 0), (89, E - 1, 76), (33, E // 2, 40)):
+        bad = g.clone()
+        bad[t, e] = float("inf")
+        got = sw.swimba_router_linear_bwd(u, W, bad)
+        assert torch.equal(got.du[t], torch.sign(W[e].float()).to(u.dtype) * float("inf"))
+        assert torch.equal(got.dW_g[e], torch.sign(u[t].float()) * float("inf"))
+        got.du[t], got.dW_g[e] = want.du[t], want.dW_g[e]
+        assert torch.equal(got.du, want.du) and torch.equal(got.dW_g, want.dW_g)
+        bad = W.clone()
+        bad[e, c] = float("-inf")
+        got = sw.swimba_router_linear_bwd(u, bad, g)
+        assert torch.equal(got.du[:, c], torch.sign(g[:, e].float()).to(u.dtype) * float("-inf"))
+        got.du[:, c] = want.du[:, c]
+        assert torch.equal(got.du, want.du) and torch.equal(got.dW_g, want.dW_g)
+
+
 def test_linear_backward_keeps_rows_apart():
     """Values that are no numbers reach their own row of du and, in a feature, their own column of dW_g."""
     u, W, g, _ = linear_case(400, 300, 10, "bf16", 3)
