@@ -247,27 +247,35 @@ norm_reduce_kernel(const float *__restrict__ part, int rows, int D, float *__res
 
 namespace {
 
-// Lanes of a row: one piece to a lane up to 256 features, 16 elements at most beyond.
-int lanes_per_row(int D) { return D <= 64 ? 16 : D <= 128 ? 32 : D <= 1024 ? 64 : D <= 4096 ? 256 : D <= 8192 ? 512 : 1024; }
+// Lanes of a row: one piece to a lane up to 256 features; beyond, 16 elements at most, or 24 where that keeps more lanes at work
+// (bf16 rows of 5204: 59.6 us with 512 lanes, 47.3 with 256; of 9000 69.7 with 1024, 49.2 with 512; backward 99.5, 78.3 and 72.9,
+// 48.0).  Four-byte rows of 4096 to 6144 gain nothing by it, and their backward pass has no registers for it.
+int lanes_per_row(int D, bool bf, bool back)
+{
+    if (D <= 1024) return D <= 64 ? 16 : D <= 128 ? 32 : 64;
+    return D <= (bf ? 6144 : 4096) ? 256 : D <= (bf || !back ? 12288 : 8192) ? 512 : 1024;
+}
 
 // f(elements of a piece, pieces, lanes of a row, whether the last piece may be short) as constants.  Pieces of 16 bytes for
 // wide rows of bf16 alone (32768 x 2048 forward 62 us with 8 bytes, 58.6 with 16; backward 85 and 79); of 4 elements elsewhere,
 // which fill the lanes of a narrow row better.
-template <typename T, typename R, typename F>
+template <typename T, typename R, bool BACK, typename F>
 void with_row(int D, F &&f)
 {
     using std::integral_constant;
+    constexpr bool BF = sizeof(T) + sizeof(R) == 4;
     constexpr integral_constant<int, 1> one;
     constexpr integral_constant<int, 2> two;
     constexpr integral_constant<int, 3> three;
     constexpr integral_constant<int, 4> four;
-    constexpr integral_constant<int, sizeof(T) + sizeof(R) == 4 ? 8 : 4> wide;
+    constexpr integral_constant<int, BF ? 8 : 4> wide;
     constexpr integral_constant<int, 16 / wide> most;
+    constexpr integral_constant<int, 24 / wide> more;
     auto tail = [&](auto w, auto pieces, auto lanes) {
         if (D % w) f(w, pieces, lanes, std::true_type());
         else f(w, pieces, lanes, std::false_type());
     };
-    switch (lanes_per_row(D)) {
+    switch (lanes_per_row(D, BF, BACK)) {
     case 16: return tail(four, one, integral_constant<int, 16>());
     case 32: return tail(four, one, integral_constant<int, 32>());
     case 64: {
@@ -276,9 +284,18 @@ void with_row(int D, F &&f)
     }
     case 256: {
         constexpr integral_constant<int, 256> lanes;
+        if constexpr (BF) {
+            if (D > 4096) return tail(wide, more, lanes);
+        }
         return D <= 2048 ? tail(wide, integral_constant<int, most / 2>(), lanes) : tail(wide, most, lanes);
     }
-    case 512: return tail(wide, most, integral_constant<int, 512>());
+    case 512: {
+        constexpr integral_constant<int, 512> lanes;
+        if constexpr (BF || !BACK) {
+            if (D > 8192) return tail(wide, more, lanes);
+        }
+        return tail(wide, most, lanes);
+    }
     default: return tail(wide, most, integral_constant<int, 1024>());
     }
 }
@@ -298,17 +315,18 @@ swimba_status norm_fwd(int64_t tokens, int D, const void *x, const void *residua
                            dim3(norm_threads(lpr)), 0, st, (const T *)x, (const R *)residual, gamma, beta, eps, (T *)u, (R *)sum, mean,
                            rstd, tokens, D);
     };
-    with_row<T, R>(D, go);
+    with_row<T, R, false>(D, go);
     SWIMBA_CHECK_LAUNCH();
     return SWIMBA_OK;
 }
 
 // Blocks of the backward pass, which keep sums of their own: one, whose sums need no second launch, for up to four rounds of
-// its rows.
+// its rows; no more than two to a compute unit, or one for the widest rows.  The same for all types: only rows of more than a wave
+// lie in other numbers of lanes, one of them to a block.
 int64_t bwd_blocks(int64_t tokens, int D)
 {
-    const int lpr = lanes_per_row(D), rpb = bwd_threads(lpr, (D + 4 * lpr - 1) / (4 * lpr)) / lpr;
-    return tokens <= 4 * rpb ? (tokens > 0) : blocks_for(tokens, rpb, lanes_per_row(D) == 1024 ? 256 : 512);
+    const int lpr = lanes_per_row(D, true, true), rpb = bwd_threads(lpr, (D + 4 * lpr - 1) / (4 * lpr)) / lpr;
+    return tokens <= 4 * rpb ? (tokens > 0) : blocks_for(tokens, rpb, D > 8192 ? 256 : 512);
 }
 
 template <typename T, typename R>
@@ -320,7 +338,7 @@ swimba_status norm_bwd(int64_t tokens, int D, const void *du, const void *r, con
                            dim3(bwd_threads(lpr, nv)), 0, st, (const T *)du, (const R *)r, gamma, mean, rstd, (const R *)d_sum, (R *)dx,
                            (T *)dx_io, pgamma, pbeta, tokens, D);
     };
-    with_row<T, R>(D, go);
+    with_row<T, R, true>(D, go);
     SWIMBA_CHECK_LAUNCH();
     return SWIMBA_OK;
 }

@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 
 # both sides of every width at which another number of lanes or waves takes a row, and rows that start at any element
 WIDTHS = [1, 2, 7, 8, 9, 16, 63, 64, 65, 100, 127, 128, 129, 256, 257, 504, 511, 512, 513, 768, 1001, 1024, 1025, 2047,
-          2048, 2056, 4096, 4099, 8192, 8200, 12345, 16384]
+          2048, 2056, 4096, 4099, 6144, 6145, 8192, 8200, 12288, 12345, 16384]
 TYPES = [("f32", None), ("bf16", None), ("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")]
 
 
