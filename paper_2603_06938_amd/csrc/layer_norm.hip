@@ -2,7 +2,10 @@
 //   forward   r = x (+ residual, rounded to the type it is stored in), u = (r - m) s gamma + beta
 //   backward  dx = s (g - mean g - xh mean(g xh)) + d_sum with g = du gamma, xh = (r - m) s;  dgamma = sum_t du xh, dbeta = sum_t du
 // Both are bound by memory: every row is read once into registers, where the mean, then the centred squares (or both sums of
-// the backward pass) are taken in fp32, and written once.
+// the backward pass) are taken in fp32, and written once.  16384 x 768 of bf16 into an fp32 stream 25.6 us (151 MB, 5.9 TB/s),
+// back 38.9 (201 MB, 5.2 TB/s); 32768 x 4096 of bf16 118 us (4.5 TB/s), back 153 (5.3 TB/s); one token 2.1 us of kernel.
+// Where a row does not end with a piece, the last one is moved to end with it: 20490 x 2047 of bf16 back 83 us, 131 with loads by
+// element, of which each waits for the one before.
 #include "rows.hpp"
 
 namespace swimba {
@@ -11,6 +14,19 @@ namespace swimba {
 // lane l are the elements from W (l + LPR i) on.
 constexpr int norm_threads(int LPR) { return LPR < 256 ? 256 : LPR; }
 constexpr int rows_per_block(int LPR) { return norm_threads(LPR) / LPR; }
+
+// Pieces that end before the narrowest row of those that LPR lanes with NV pieces are chosen for.
+constexpr int whole_pieces(int LPR, int NV) { return LPR <= 64 || NV < 4 ? NV - 1 : NV - 2; }
+
+// Piece i of a lane.  Where it may be moved, its place is worked out anew wherever it is asked for: kept for all pieces, the places
+// would take the registers of a wave.
+template <Tail TAIL, int W, int LPR, int NV> __device__ __forceinline__ Part<TAIL, W> row_part(int lane, int i, int D)
+{
+    const bool whole = i < whole_pieces(LPR, NV);
+    uint32_t from = W * (lane + LPR * i);
+    if (TAIL == MOVED && !whole) asm volatile("" : "+v"(from));
+    return Part<TAIL, W>(from, D, whole);
+}
 
 // Threads of a block of the backward pass, of which two fit on a compute unit at the registers that its pieces take.
 constexpr int bwd_threads(int LPR, int NV) { return LPR > 64 ? LPR : NV == 1 ? 1024 : NV == 2 ? 512 : 256; }
@@ -41,7 +57,7 @@ template <int LPR> __device__ __forceinline__ int row_slot()
     return LPR < 64 ? threadIdx.x / LPR : __builtin_amdgcn_readfirstlane(threadIdx.x / 64) / (LPR / 64);
 }
 
-template <typename T, typename R, int W, int NV, int LPR, bool TAIL>
+template <typename T, typename R, int W, int NV, int LPR, Tail TAIL>
 __global__ void __launch_bounds__(norm_threads(LPR))
 norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
                 T *__restrict__ u, R *sum, float *__restrict__ mean, float *__restrict__ rstd, int64_t tokens, int D)
@@ -50,15 +66,16 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
     constexpr int RPB = rows_per_block(LPR);                   // rows a block has at a time
     const int lane = threadIdx.x % LPR;
     const float width = (float)D;
+    auto part = [&](int i) __attribute__((always_inline)) { return row_part<TAIL, W, LPR, NV>(lane, i, D); };
     int round = 0;
     // Gain and bias are under way with the row where it lies in one wave (16384 x 768 13.0 -> 11.0 us); more lanes to a row have
     // other waves to wait with and lose by the registers (16384 x 8192 118 -> 136 us).
     constexpr bool EARLY = LPR <= 64;
     Piece<float, W> g[EARLY ? NV : 1], b[EARLY ? NV : 1];
     auto weights = [&](int i, int k) __attribute__((always_inline)) {
-        const uint32_t d = W * (lane + LPR * i);
-        if (gamma) g[k].template load<TAIL>(gamma + d, D - (int)d);
-        if (beta) b[k].template load<TAIL>(beta + d, D - (int)d);
+        const auto at = part(i);
+        if (gamma) at.load(g[k], gamma);
+        if (beta) at.load(b[k], beta);
     };
     if constexpr (EARLY) {
 #pragma unroll
@@ -73,32 +90,32 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
         Piece<R, W> pr[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t d = W * (lane + LPR * i);
-            px[i].template load<TAIL>(xr + d, D - (int)d);
-            if (residual) pr[i].template load<TAIL>(rr + d, D - (int)d);
+            const auto at = part(i);
+            at.load(px[i], xr);
+            if (residual) at.load(pr[i], rr);
         }
         float r[NV][W], s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t d = W * (lane + LPR * i);
+            const auto at = part(i);
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 r[i][j] = px[i].get(j);
                 if (residual) r[i][j] = to_float(from_float<R>(r[i][j] + pr[i].get(j)));
-                s[0] += r[i][j];
+                s[0] += TAIL != MOVED || at.own(j) ? r[i][j] : 0.f;
             }
-            if (sum) store_piece<TAIL>(sr + d, r[i], D - (int)d);
+            if (sum) at.store(sr, r[i]);
         }
         row_sums<LPR>(s, lds, round++);
         const float m = s[0] / width;                          // divided, not multiplied: a constant row is centred to zero
         s[0] = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int n = D - W * (lane + LPR * i);
+            const auto at = part(i);
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 r[i][j] -= m;
-                s[0] += j < n ? r[i][j] * r[i][j] : 0.f;
+                s[0] += at.own(j) ? r[i][j] * r[i][j] : 0.f;
             }
         }
         row_sums<LPR>(s, lds, round++);
@@ -109,37 +126,36 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t d = W * (lane + LPR * i);
             const int k = EARLY ? i : 0;
             if constexpr (!EARLY) weights(i, 0);
 #pragma unroll
             for (int j = 0; j < W; ++j) r[i][j] = r[i][j] * is * (gamma ? g[k].get(j) : 1.f) + (beta ? b[k].get(j) : 0.f);
-            store_piece<TAIL>(ur + d, r[i], D - (int)d);
+            part(i).store(ur, r[i]);
         }
     }
 }
 
 // The blocks keep sums of their own for dgamma and dbeta: part (blocks, 2, D), or the two themselves where there is one block.
-template <typename T, typename R, int W, int NV, int LPR, bool TAIL>
+template <typename T, typename R, int W, int NV, int LPR, Tail TAIL>
 __global__ void __launch_bounds__(bwd_threads(LPR, NV))
 norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *__restrict__ gamma,
                 const float *__restrict__ mean, const float *__restrict__ rstd, const R *d_sum, R *dx, T *__restrict__ dx_io,
                 float *__restrict__ pgamma, float *__restrict__ pbeta, int64_t tokens, int D)
 {
     constexpr int THREADS = bwd_threads(LPR, NV), RPB = THREADS / LPR, SPAN = LPR * W;
-    constexpr bool AHEAD = LPR < 1024;                         // 1024 threads have no registers for it, nor for the gain
+    constexpr bool AHEAD = NV * W <= (sizeof(T) + sizeof(R) == 4 ? 24 : 16);   // more leave no registers for it, nor for the gain
     __shared__ float lds[2][2][16];
     __shared__ float comb[RPB > 1 ? RPB * 2 * NV * SPAN : 1];
     const int lane = threadIdx.x % LPR, slot = row_slot<LPR>();
     const float width = (float)D;
+    auto part = [&](int i) __attribute__((always_inline)) { return row_part<TAIL, W, LPR, NV>(lane, i, D); };
     const int64_t stride = (int64_t)gridDim.x * RPB;
     float dg[NV][W] = {}, db[NV][W] = {}, w[NV][W];
     auto gain = [&] {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t d = W * lane + SPAN * i;
             Piece<float, W> p;
-            if (gamma) p.template load<TAIL>(gamma + d, D - (int)d);
+            if (gamma) part(i).load(p, gamma);
 #pragma unroll
             for (int j = 0; j < W; ++j) w[i][j] = gamma ? p.get(j) : 1.f;
         }
@@ -157,10 +173,10 @@ norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *
         const T *const grad = du + t * D;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t d = W * lane + SPAN * i;
-            q.x[i].template load<TAIL>(row + d, D - (int)d);
-            q.g[i].template load<TAIL>(grad + d, D - (int)d);
-            if (AHEAD && d_sum) q.a[i].template load<TAIL>(add + d, D - (int)d);
+            const auto at = part(i);
+            at.load(q.x[i], row);
+            at.load(q.g[i], grad);
+            if (AHEAD && d_sum) at.load(q.a[i], add);
         }
     };
     Row next;
@@ -178,11 +194,11 @@ norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *
         float xh[NV][W], g[NV][W], s[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int n = D - (W * lane + SPAN * i);
+            const auto at = part(i);
 #pragma unroll
             for (int j = 0; j < W; ++j) {
-                xh[i][j] = j < n ? (q.x[i].get(j) - q.m) * q.s : 0.f;
-                g[i][j] = q.g[i].get(j);
+                xh[i][j] = at.own(j) ? (q.x[i].get(j) - q.m) * q.s : 0.f;
+                g[i][j] = TAIL != MOVED || at.own(j) ? q.g[i].get(j) : 0.f;
                 dg[i][j] += g[i][j] * xh[i][j];
                 db[i][j] += g[i][j];
                 g[i][j] *= w[i][j];
@@ -197,25 +213,28 @@ norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *
         const R *const add = d_sum + t * D;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t d = W * lane + SPAN * i;
-            if (!AHEAD && d_sum) q.a[i].template load<TAIL>(add + d, D - (int)d);
+            const auto at = part(i);
+            if (!AHEAD && d_sum) at.load(q.a[i], add);
 #pragma unroll
             for (int j = 0; j < W; ++j) g[i][j] = q.s * (g[i][j] - mg - xh[i][j] * mx) + (d_sum ? q.a[i].get(j) : 0.f);
-            store_piece<TAIL>(out + d, g[i], D - (int)d);
-            if (dx_io) store_piece<TAIL>(out_io + d, g[i], D - (int)d);
+            at.store(out, g[i]);
+            if (dx_io) at.store(out_io, g[i]);
         }
     }
     float *const pg = pgamma + (int64_t)blockIdx.x * 2 * D, *const pb = pbeta + (int64_t)blockIdx.x * 2 * D;
     if (!pgamma && !pbeta) return;
     if constexpr (RPB > 1) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            const auto at = part(i);
 #pragma unroll
             for (int j = 0; j < W; ++j) {
-                const int d = W * lane + SPAN * i + j;
+                if (!at.own(j)) continue;
+                const int d = at.at + j;
                 comb[(slot * 2) * NV * SPAN + d] = dg[i][j];
                 comb[(slot * 2 + 1) * NV * SPAN + d] = db[i][j];
             }
+        }
         __syncthreads();
         for (int c = threadIdx.x; c < 2 * D; c += THREADS) {
             const int at = c < D ? c : c - D + NV * SPAN;
@@ -228,9 +247,8 @@ norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *
     } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t d = W * lane + SPAN * i;
-            if (pgamma) store_piece<TAIL>(pg + d, dg[i], D - (int)d);
-            if (pbeta) store_piece<TAIL>(pb + d, db[i], D - (int)d);
+            if (pgamma) part(i).store(pg, dg[i]);
+            if (pbeta) part(i).store(pb, db[i]);
         }
     }
 }
@@ -248,15 +266,16 @@ norm_reduce_kernel(const float *__restrict__ part, int rows, int D, float *__res
 namespace {
 
 // Lanes of a row: one piece to a lane up to 256 features; beyond, 16 elements at most, or 24 where that keeps more lanes at work
-// (bf16 rows of 5204: 59.6 us with 512 lanes, 47.3 with 256; of 9000 69.7 with 1024, 49.2 with 512; backward 99.5, 78.3 and 72.9,
-// 48.0).  Four-byte rows of 4096 to 6144 gain nothing by it, and their backward pass has no registers for it.
+// (bf16 rows of 5204: 59.6 us with 512 lanes, 47.3 with 256; of 9000 69.7 with 1024, 49.2 with 512).  Four-byte rows of 4096 to
+// 6144 gain nothing by it.  The backward pass has up to 32 in 512 lanes, without the next row under way: 1024 have 128 registers
+// each and spill (2560 x 16384 fp32 104 us, 96 with 512; 4660 x 9000 113 and 94).
 int lanes_per_row(int D, bool bf, bool back)
 {
     if (D <= 1024) return D <= 64 ? 16 : D <= 128 ? 32 : 64;
-    return D <= (bf ? 6144 : 4096) ? 256 : D <= (bf || !back ? 12288 : 8192) ? 512 : 1024;
+    return D <= (bf ? 6144 : 4096) ? 256 : D <= 12288 || back ? 512 : 1024;
 }
 
-// f(elements of a piece, pieces, lanes of a row, whether the last piece may be short) as constants.  Pieces of 16 bytes for
+// f(elements of a piece, pieces, lanes of a row, how the last piece is read) as constants.  Pieces of 16 bytes for
 // wide rows of bf16 alone (32768 x 2048 forward 62 us with 8 bytes, 58.6 with 16; backward 85 and 79); of 4 elements elsewhere,
 // which fill the lanes of a narrow row better.
 template <typename T, typename R, bool BACK, typename F>
@@ -272,8 +291,11 @@ void with_row(int D, F &&f)
     constexpr integral_constant<int, 16 / wide> most;
     constexpr integral_constant<int, 24 / wide> more;
     auto tail = [&](auto w, auto pieces, auto lanes) {
-        if (D % w) f(w, pieces, lanes, std::true_type());
-        else f(w, pieces, lanes, std::false_type());
+        if constexpr (lanes == 16) {
+            if (tail_of(D, w) == BY_ELEMENT) return f(w, pieces, lanes, integral_constant<Tail, BY_ELEMENT>());
+        }
+        if (tail_of(D, w) == MOVED) f(w, pieces, lanes, integral_constant<Tail, MOVED>());
+        else f(w, pieces, lanes, integral_constant<Tail, NO_TAIL>());
     };
     switch (lanes_per_row(D, BF, BACK)) {
     case 16: return tail(four, one, integral_constant<int, 16>());
@@ -291,12 +313,13 @@ void with_row(int D, F &&f)
     }
     case 512: {
         constexpr integral_constant<int, 512> lanes;
-        if constexpr (BF || !BACK) {
-            if (D > 8192) return tail(wide, more, lanes);
+        if constexpr (BACK) {
+            if (D > 12288) return tail(wide, integral_constant<int, 32 / wide>(), lanes);
         }
-        return tail(wide, most, lanes);
+        return D > 8192 ? tail(wide, more, lanes) : tail(wide, most, lanes);
     }
-    default: return tail(wide, most, integral_constant<int, 1024>());
+    default:
+        if constexpr (!BACK) tail(wide, most, integral_constant<int, 1024>());
     }
 }
 

@@ -89,6 +89,38 @@ template <bool TAIL, typename T, int W> __device__ __forceinline__ void store_pi
     }
 }
 
+// How a row's last piece is read, where it is shorter than the others: it is not, by element, or (in rows of a piece or more) moved
+// to end with the row, so that it has some elements of its neighbour in front of its own.  By element, a load waits for the one
+// before it, at every row.
+enum Tail { NO_TAIL, BY_ELEMENT, MOVED };
+constexpr Tail tail_of(int D, int W) { return D % W == 0 ? NO_TAIL : D < W ? BY_ELEMENT : MOVED; }
+
+// A lane's piece of a row of D: W elements that start at d, or with `whole` are there for certain.
+template <Tail TAIL, int W> struct Part {
+    const uint32_t d, at;              // where it starts, and where it is read
+    const int D;
+    const bool whole;
+    __device__ __forceinline__ Part(uint32_t from, int width, bool certain)
+        : d(from), at(TAIL == MOVED && !certain ? min(from, (uint32_t)(width - W)) : from), D(width), whole(certain) {}
+    __device__ __forceinline__ bool own(int j) const { return whole || (TAIL == MOVED ? j >= (int)(d - at) : (int)d + j < D); }
+    // elements that are not its own: a neighbour's where it is moved, zero otherwise
+    template <typename T> __device__ __forceinline__ void load(Piece<T, W> &p, const T *row) const
+    {
+        if (whole || TAIL == MOVED) p.template load<false>(row + at, W);
+        else p.template load<TAIL == BY_ELEMENT>(row + d, D - (int)d);
+    }
+    template <typename T> __device__ __forceinline__ void store(T *row, const float (&f)[W]) const
+    {
+        if (whole || (TAIL == MOVED && d == at)) store_piece<false>(row + at, f, W);
+        else if (TAIL == MOVED) {
+#pragma unroll
+            for (int j = 1; j < W; ++j)
+                if (own(j)) row[at + j] = from_float<T>(f[j]);
+        } else
+            store_piece<TAIL == BY_ELEMENT>(row + d, f, D - (int)d);
+    }
+};
+
 // out[c] = sum over `rows` rows of part (rows, n), c < n, in an order that the sizes alone decide.  32 columns to a block of 512
 // threads, whose 16 half waves take every 16th row each: a piece of a row is a line of memory, and up to 16 x 8 are under way.
 template <typename Store>
