@@ -155,9 +155,10 @@ norm_bwd_kernel(const T *__restrict__ du, const R *__restrict__ r, const float *
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             Piece<float, W> p;
-            if (gamma) part(i).load(p, gamma);
+            const auto at = part(i);
+            if (gamma) at.load(p, gamma);
 #pragma unroll
-            for (int j = 0; j < W; ++j) w[i][j] = gamma ? p.get(j) : 1.f;
+            for (int j = 0; j < W; ++j) w[i][j] = TAIL == MOVED && !at.own(j) ? 0.f : gamma ? p.get(j) : 1.f;
         }
     };
     if constexpr (AHEAD) gain();
