@@ -109,6 +109,25 @@ template <Tail TAIL, int W> struct Part {
         if (whole || TAIL == MOVED) p.template load<false>(row + at, W);
         else p.template load<TAIL == BY_ELEMENT>(row + d, D - (int)d);
     }
+    // its own elements to the places that they would have, zero behind them
+    template <typename T> __device__ __forceinline__ void settle(Piece<T, W> &p) const
+    {
+        if constexpr (TAIL == MOVED) {
+            constexpr int WORDS = Piece<T, W>::WORDS;
+            const int by = d - at;
+            if (by == 0) return;
+            const int words = by * (int)sizeof(T) / 4;
+#pragma unroll
+            for (int b = WORDS / 2; b > 0; b /= 2)
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) p.v[i] = words & b ? (i + b < WORDS ? p.v[i + b] : 0) : p.v[i];
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) {
+                if (sizeof(T) == 2) p.v[i] = by % 2 ? p.v[i] >> 16 | (i + 1 < WORDS ? p.v[i + 1] << 16 : 0) : p.v[i];
+                p.v[i] = by < W ? p.v[i] : 0;
+            }
+        }
+    }
     template <typename T> __device__ __forceinline__ void store(T *row, const float (&f)[W]) const
     {
         if (whole || (TAIL == MOVED && d == at)) store_piece<false>(row + at, f, W);
