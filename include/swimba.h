@@ -405,7 +405,7 @@ swimba_status swimba_router_linear(int64_t tokens, int32_t d_model, int32_t nexp
  *   gamma, beta (d_model) fp32 [in]        NULL = 1, 0
  *   u        (tokens, d_model) io  [out]
  *   sum      (tokens, d_model) res_dtype [out] r, where residual is given; NULL = not wanted.  May be the buffer of
- *            residual or (of one type) of x: every element is read, then written, by one lane.
+ *            residual or (of one type) of x: every element is written by the one lane that takes it into the sum.
  *   mean, rstd (tokens) fp32 [out]         m and s, what the backward pass needs; NULL = not wanted
  * res_dtype is io_dtype, or SWIMBA_F32 for a residual stream kept in fp32 beside bf16 features; without a residual it has
  * to be io_dtype.  eps > 0 and finite.  The mean and the centred squares are summed in fp32 in two passes over the row in

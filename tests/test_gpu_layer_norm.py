@@ -128,6 +128,29 @@ def test_in_place_along_the_residual_stream():
             assert all(torch.equal(a, b) for a, b in zip(got, want[0]) if a is not None)
 
 
+@pytest.mark.parametrize("io,res", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("D", [5, 67, 130, 515, 771, 1030, 2047, 4099, 5205, 8195, 9001, 12289, 16381])
+def test_in_place_where_pieces_overlap(D, io, res):
+    """Rows that do not end with a piece, whose last lane reads elements of its neighbour: in place those may be new or old."""
+    x, residual, gamma, beta = case(300, D, io, res, D)
+    want = sw.swimba_layer_norm(x, gamma, beta, 1e-5, residual, want_stats=True)
+    stream = residual.clone()
+    got = sw.swimba_layer_norm(x, gamma, beta, 1e-5, stream, sum=stream, want_stats=True)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    d_sum = rows(300, D, res, 3)
+    back = sw.swimba_layer_norm_bwd(x, want.sum, gamma, want.mean, want.rstd, d_sum)
+    got = sw.swimba_layer_norm_bwd(x, want.sum, gamma, want.mean, want.rstd, d_sum, dx=d_sum)
+    assert all(torch.equal(a, b) for a, b in zip(got, back) if a is not None)
+    # a weight that is no number reaches its own column
+    for e in {0, D // 2, D - 4, D - 1} & set(range(D)):
+        bad, worse = gamma.clone(), beta.clone()
+        bad[e], worse[e] = float("inf"), float("nan")
+        out = sw.swimba_layer_norm(x, bad, worse, 1e-5, residual, want_sum=False).u
+        assert out[:, e].isnan().all()
+        out[:, e] = want.u[:, e]
+        assert torch.equal(out, want.u)
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_rows_apart_from_their_neighbours(io):
     """A row that is not finite, one that is constant, one of large offset: each reaches its own outputs alone."""
