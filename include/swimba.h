@@ -408,8 +408,10 @@ swimba_status swimba_router_linear(int64_t tokens, int32_t d_model, int32_t nexp
  *            residual or (of one type) of x: every element is written by the one lane that takes it into the sum.
  *   mean, rstd (tokens) fp32 [out]         m and s, what the backward pass needs; NULL = not wanted
  * res_dtype is io_dtype, or SWIMBA_F32 for a residual stream kept in fp32 beside bf16 features; without a residual it has
- * to be io_dtype.  eps > 0 and finite.  The mean and the centred squares are summed in fp32 in two passes over the row in
- * registers, so an offset that is large beside the deviations costs what storing the row costs and no more.  A row that is
+ * to be io_dtype.  eps > 0 and finite.  Two passes over the row in registers: the mean (of fp32 rows in 64 bits, and used
+ * unrounded), then the centred squares in fp32, so an offset that is large beside the deviations costs what storing the row
+ * costs and no more; a constant row comes out as beta.  (The backward pass takes the mean as it is stored, rounded.)  Rows
+ * whose summed squares pass the range of fp32, deviations of some 10^17 and more, get s = 0.  A row that is
  * not finite reaches nothing but its own outputs.  d_model up to SWIMBA_MAX_DMODEL_GENERIC.  Large tensors
  * 16-byte aligned, gamma, beta, mean and rstd by element; rows need no alignment of their own.  No workspace, one launch.
  */

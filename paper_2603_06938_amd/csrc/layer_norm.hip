@@ -1,8 +1,8 @@
 // Layer norm of token features and its backward pass.
 //   forward   r = x (+ residual, rounded to the type it is stored in), u = (r - m) s gamma + beta
 //   backward  dx = s (g - mean g - xh mean(g xh)) + d_sum with g = du gamma, xh = (r - m) s;  dgamma = sum_t du xh, dbeta = sum_t du
-// Both are bound by memory: every row is read once into registers, where the mean, then the centred squares (or both sums of
-// the backward pass) are taken in fp32, and written once.  16384 x 768 of bf16 into an fp32 stream 25.6 us (151 MB, 5.9 TB/s),
+// Both are bound by memory: every row is read once into registers, where the mean (of fp32 rows in 64 bits), then the centred
+// squares (or both sums of the backward pass) are taken in fp32, and written once.  16384 x 768 of bf16 into an fp32 stream 25.6 us (151 MB, 5.9 TB/s),
 // back 38.9 (201 MB, 5.2 TB/s); 32768 x 4096 of bf16 118 us (4.5 TB/s), back 153 (5.3 TB/s); one token 2.1 us of kernel.
 // Where a row does not end with a piece, the last one is moved to end with it: 20490 x 2047 of bf16 back 83 us, 131 with loads by
 // element, of which each waits for the one before.
@@ -51,6 +51,20 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[N][16], int
     }
 }
 
+// the same of one value, in 64 bits
+template <int LPR> __device__ __forceinline__ double row_sum(double v, double (*lds)[16], int round)
+{
+    v = group_sum<LPR < 64 ? LPR : 64>(v);
+    if constexpr (LPR > 64) {
+        lds[round & 1][threadIdx.x >> 6] = v;
+        lds_barrier();
+        v = 0.;
+#pragma unroll
+        for (int w = 0; w < LPR / 64; ++w) v += lds[round & 1][w];
+    }
+    return v;
+}
+
 // first row of the thread's lanes in the block
 template <int LPR> __device__ __forceinline__ int row_slot()
 {
@@ -60,9 +74,15 @@ template <int LPR> __device__ __forceinline__ int row_slot()
 template <typename T, typename R, int W, int NV, int LPR, Tail TAIL>
 __global__ void __launch_bounds__(norm_threads(LPR))
 norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
-                T *__restrict__ u, R *sum, float *__restrict__ mean, float *__restrict__ rstd, int64_t tokens, int D)
+                T *__restrict__ u, R *sum, float *__restrict__ mean, float *__restrict__ rstd, int64_t tokens, int D, double per_width)
 {
+    // What a mean is off by shifts every deviation, and its square goes into the variance.  Rows of bf16 are summed in 32 bits:
+    // equal elements exactly (8 bits each, at most 2^14 of them), others to some 2^-18 of the largest, where each is stored to 2^-9.
+    // Rows of fp32 are summed in 64, and what the mean loses in 32 bits is taken off the deviations as well; in 32 bits a row of
+    // 1000 times 12345.678 would come out at 0.5 instead of 0 (no slower: 16384 x 1024 22.8 us, 16384 x 4096 96; 4096 x 16384 120, 118 in 32 bits).
+    constexpr bool WIDE = sizeof(R) == 4;
     __shared__ float lds[2][1][16];
+    __shared__ double lds64[2][16];
     constexpr int RPB = rows_per_block(LPR);                   // rows a block has at a time
     const int lane = threadIdx.x % LPR;
     const float width = (float)D;
@@ -94,7 +114,8 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
             at.load(px[i], xr);
             if (residual) at.load(pr[i], rr);
         }
-        float r[NV][W], s[1] = {0.f};
+        float r[NV][W], s[1];
+        std::conditional_t<WIDE, double, float> total = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const auto at = part(i);
@@ -102,12 +123,22 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
             for (int j = 0; j < W; ++j) {
                 r[i][j] = px[i].get(j);
                 if (residual) r[i][j] = to_float(from_float<R>(r[i][j] + pr[i].get(j)));
-                s[0] += TAIL != MOVED || at.own(j) ? r[i][j] : 0.f;
+                total += TAIL != MOVED || at.own(j) ? r[i][j] : 0.f;
             }
             if (sum) at.store(sr, r[i]);
         }
-        row_sums<LPR>(s, lds, round++);
-        const float m = s[0] / width;                          // divided, not multiplied: a constant row is centred to zero
+        float m, rest = 0.f;                                   // the mean, and what it has beyond 32 bits
+        if constexpr (WIDE) {
+            const double all = row_sum<LPR>(total, lds64, round++);
+            double q = all * per_width;
+            q = fma(fma(-q, (double)D, all), per_width, q);    // divided, so that a constant row is centred to zero
+            m = (float)q;
+            rest = (float)(q - m);
+        } else {
+            s[0] = total;
+            row_sums<LPR>(s, lds, round++);
+            m = s[0] / width;
+        }
         s[0] = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -115,6 +146,7 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 r[i][j] -= m;
+                if constexpr (WIDE) r[i][j] -= rest;
                 s[0] += at.own(j) ? r[i][j] * r[i][j] : 0.f;
             }
         }
@@ -337,7 +369,7 @@ swimba_status norm_fwd(int64_t tokens, int D, const void *x, const void *residua
     auto go = [&](auto w, auto nv, auto lpr, auto tail) {
         hipLaunchKernelGGL((norm_fwd_kernel<T, R, w(), nv(), lpr(), tail()>), dim3((unsigned)blocks_for(tokens, rows_per_block(lpr), 1 << 20)),
                            dim3(norm_threads(lpr)), 0, st, (const T *)x, (const R *)residual, gamma, beta, eps, (T *)u, (R *)sum, mean,
-                           rstd, tokens, D);
+                           rstd, tokens, D, 1. / D);
     };
     with_row<T, R, false>(D, go);
     SWIMBA_CHECK_LAUNCH();

@@ -201,6 +201,21 @@ __device__ __forceinline__ uint32_t max_f32(uint32_t a, uint32_t b) { return __f
 __device__ __forceinline__ uint32_t add_u32(uint32_t a, uint32_t b) { return a + b; }
 __device__ __forceinline__ uint32_t or_u32(uint32_t a, uint32_t b) { return a | b; }
 template <int G> __device__ __forceinline__ float group_sum(float v) { return __uint_as_float(over_group<G>(__float_as_uint(v), add_f32)); }
+// the same in 64 bits, whose halves move one after the other; D: distance of the step
+template <int G, int D = 1> __device__ __forceinline__ double group_sum(double v)
+{
+    if constexpr (D < G) {
+        const uint32_t lo = (uint32_t)__double2loint(v), hi = (uint32_t)__double2hiint(v);
+        if constexpr (D >= 16) {
+            const auto a = D == 16 ? __builtin_amdgcn_permlane16_swap(lo, lo, false, false) : __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
+            const auto b = D == 16 ? __builtin_amdgcn_permlane16_swap(hi, hi, false, false) : __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+            v = __hiloint2double((int)b[0], (int)a[0]) + __hiloint2double((int)b[1], (int)a[1]);
+        } else
+            v += __hiloint2double((int)partner<D>(hi), (int)partner<D>(lo));
+        return group_sum<G, 2 * D>(v);
+    }
+    return v;
+}
 
 // Sums of N values over the lanes whose numbers differ in the bits from G to below 2 D.  While a lane has several, a step halves
 // them: the lanes with bit D clear keep the lower half, the others the upper.  v[i] is then the sum of value `first` + i.
