@@ -431,7 +431,7 @@ swimba_status swimba_layer_norm(int64_t tokens, int32_t d_model, int32_t io_dtyp
  *            wanted, and refused where the types are equal (dx is it)
  *   dgamma, dbeta (d_model) fp32 [out]     NULL = not wanted
  * The sums over the tokens are taken in fp32 in an order that sizes alone decide (zero for no tokens).
- *   workspace >= swimba_layer_norm_bwd_workspace_bytes(tokens, d_model), 256-byte aligned.
+ *   workspace >= swimba_layer_norm_bwd_workspace_bytes(tokens, d_model), 256-byte aligned; enough for fewer tokens, too.
  *            Where that is 256, its smallest, nothing is kept there and it may be NULL.
  */
 size_t swimba_layer_norm_bwd_workspace_bytes(int64_t tokens, int32_t d_model);
@@ -455,7 +455,8 @@ swimba_status swimba_layer_norm_bwd(int64_t tokens, int32_t d_model, int32_t io_
  *   counts   (groups, E) int32 [out]    prob_mean (groups, E) fp32 [out]  NULL = not wanted    loss (groups) fp32 [out]
  * A logit that is NaN or +inf in a token that counts makes the probabilities and the loss of its group NaN.
  * At most 2^20 groups, 2^31 - 1 tokens to a group and 2^38 in all.  Element-aligned pointers, rows of any width.
- *   workspace >= swimba_router_balance_workspace_bytes(groups, tokens, nexperts), 256-byte aligned.
+ *   workspace >= swimba_router_balance_workspace_bytes(groups, tokens, nexperts), 256-byte aligned; enough for fewer tokens,
+ *            too, and, of up to 128 groups, for fewer groups (more of them keep nothing there).
  *            Where that is 256, its smallest, nothing is kept there and it may be NULL.
  */
 size_t swimba_router_balance_workspace_bytes(int64_t groups, int64_t tokens, int32_t nexperts);
@@ -491,7 +492,8 @@ swimba_status swimba_router_bwd(int64_t groups, int64_t tokens, int32_t nexperts
  * fp32 accumulation; du is rounded once, dW_g is not rounded, its sum over the tokens is taken in an order that sizes alone decide.
  * u is read for dW_g only, W_g for du only; the other may be NULL.  Limits and alignment (du, du_add as u) as in
  * swimba_router_linear, rows of any width; dW_g by element.
- *   workspace >= swimba_router_linear_bwd_workspace_bytes(tokens, d_model, nexperts), 256-byte aligned.
+ *   workspace >= swimba_router_linear_bwd_workspace_bytes(tokens, d_model, nexperts), 256-byte aligned; enough for fewer
+ *            tokens, too.
  *            Where that is 256, its smallest, nothing is kept there and it may be NULL.
  */
 size_t swimba_router_linear_bwd_workspace_bytes(int64_t tokens, int32_t d_model, int32_t nexperts);

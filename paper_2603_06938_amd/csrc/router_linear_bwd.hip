@@ -287,12 +287,19 @@ linear_reduce_kernel(const float *__restrict__ part, int rows, int64_t n, float 
 
 namespace {
 
-// Shares of whole steps (`step` tokens), as many as bring the blocks, `per_share` of them to a share, to `want`.
-Shares shares_of(int64_t tokens, int64_t per_share, int64_t step, int64_t want)
+// Shares of whole steps (`step` tokens), as many as bring the blocks, `per_share` of them to a share, to `want`: that many at
+// most, a number that does not fall as the tokens grow, and what is left of them where a share is the same number of steps for all.
+int64_t most_shares(int64_t tokens, int64_t per_share, int64_t step, int64_t want)
 {
     const int64_t most = per_share < want ? want / per_share : 1, steps = (tokens + step - 1) / step;
-    const int64_t count = steps < most ? (steps > 0 ? steps : 1) : most, share = (steps + count - 1) / count * step;
-    return {share, tokens > 0 ? (tokens + share - 1) / share : 0};
+    return steps < most ? steps : most;
+}
+Shares shares_of(int64_t tokens, int64_t per_share, int64_t step, int64_t want)
+{
+    if (tokens == 0) return {step, 0};
+    const int64_t steps = (tokens + step - 1) / step, count = most_shares(tokens, per_share, step, want);
+    const int64_t share = (steps + count - 1) / count * step;
+    return {share, (tokens + share - 1) / share};
 }
 int experts_of(int E) { return E <= 16 ? 16 : E <= 32 ? 32 : 64; }                 // of a block of dW
 // Blocks that sum dW, half of those that the chip holds at once at the kernels' registers: of two to a compute unit in fp32 and
@@ -302,10 +309,10 @@ int experts_of(int E) { return E <= 16 ? 16 : E <= 32 ? 32 : 64; }              
 // memory run to the end (16384 x 2048 x 16: 30.1 us, 34.6 with as many as dW has; x 64 35.1 and 41.5).
 int64_t blocks_of(int E, int element) { return element == 4 || E > 32 ? 256 : E > 16 ? 512 : 384; }
 int64_t dw_per_share(int D, int E) { return (int64_t)((D + LB_COLS - 1) / LB_COLS) * ((E + experts_of(E) - 1) / experts_of(E)); }
-// (in steps of bf16 tokens, of which those of fp32 are half)
+constexpr int DW_STEP = dw_step<bf16>() * LB_WAVES;                                 // of a block in bf16; in fp32 half of it
 Shares dw_shares(int64_t tokens, int D, int E, int element)
 {
-    return shares_of(tokens, dw_per_share(D, E), dw_step<bf16>() * LB_WAVES, blocks_of(E, element));
+    return shares_of(tokens, dw_per_share(D, E), DW_STEP, blocks_of(E, element));
 }
 
 template <typename T>
@@ -347,10 +354,10 @@ swimba_status linear_bwd(int64_t tokens, int D, int E, const void *u, const void
 
 }  // namespace
 
-// (for bf16, which has as many shares as fp32 or more)
+// For bf16, which has as many shares as fp32 or more, and for fewer tokens as well, which may have more of smaller shares.
 size_t router_linear_bwd_bytes(int64_t tokens, int D, int E)
 {
-    const int64_t n = dw_shares(tokens, D, E, 2).count;
+    const int64_t n = most_shares(tokens, dw_per_share(D, E), DW_STEP, blocks_of(E, 2));
     return n > 1 ? (size_t)n * E * D * sizeof(float) : 0;
 }
 
