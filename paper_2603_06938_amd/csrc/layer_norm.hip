@@ -131,7 +131,8 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
         if constexpr (WIDE) {
             const double all = row_sum<LPR>(total, lds64, round++);
             double q = all * per_width;
-            q = fma(fma(-q, (double)D, all), per_width, q);    // divided, so that a constant row is centred to zero
+            const double off = fma(-q, (double)D, all);        // divided, so that a constant row is centred to zero
+            q = off == off ? fma(off, per_width, q) : q;       // (an infinite row's mean stays infinite)
             m = (float)q;
             rest = (float)(q - m);
         } else {
