@@ -2,10 +2,12 @@
 //   forward   r = x (+ residual, rounded to the type it is stored in), u = (r - m) s gamma + beta
 //   backward  dx = s (g - mean g - xh mean(g xh)) + d_sum with g = du gamma, xh = (r - m) s;  dgamma = sum_t du xh, dbeta = sum_t du
 // Both are bound by memory: every row is read once into registers, where the mean (of fp32 rows in 64 bits), then the centred
-// squares (or both sums of the backward pass) are taken in fp32, and written once.  16384 x 768 of bf16 into an fp32 stream 25.6 us (151 MB, 5.9 TB/s),
-// back 38.9 (201 MB, 5.2 TB/s); 32768 x 4096 of bf16 118 us (4.5 TB/s), back 153 (5.3 TB/s); one token 2.1 us of kernel.
-// Where a row does not end with a piece, the last one is moved to end with it: 20490 x 2047 of bf16 back 83 us, 131 with loads by
-// element, of which each waits for the one before.
+// squares (or both sums of the backward pass) are taken in fp32, and written once.  16384 x 768 of bf16 into an fp32 stream
+// 25.3 us (151 MB, 6.0 TB/s), back 39.5 (201 MB, 5.1 TB/s); 32768 x 4096 of bf16 114 us (4.7 TB/s), back 153 (5.3 TB/s); one token
+// 2.4 us of kernel.
+// Where a row does not end with a piece, the last one is moved to end with it: 20490 x 2047 of bf16 back 84 us, 131 with loads by
+// element, of which each waits for the one before.  2048 wide takes 51: the moved lane's stores by element cost 22 us at 2044 to 2046
+// wide (74), rows that start inside a dword 10 more.
 #include "rows.hpp"
 
 namespace swimba {
@@ -300,7 +302,8 @@ norm_reduce_kernel(const float *__restrict__ part, int rows, int D, float *__res
 namespace {
 
 // Lanes of a row: one piece to a lane up to 256 features; beyond, 16 elements at most, or 24 where that keeps more lanes at work
-// (bf16 rows of 5204: 59.6 us with 512 lanes, 47.3 with 256; of 9000 69.7 with 1024, 49.2 with 512).  Four-byte rows of 4096 to
+// (42 million elements of bf16, 24 and 16 to a lane: rows of 4104 39.3 us and 51.0, 5204 36.7 and 46.7, 6144 33.5 and 39.0, 8200 47.9 and
+// 68.1, 10240 41.5 and 57.7, 12288 38.4 and 53.9; back 4104 51.6 and 62.9, 5204 55.3 and 71.0, 6144 the same).  Four-byte rows of 4096 to
 // 6144 gain nothing by it.  The backward pass has up to 32 in 512 lanes, without the next row under way: 1024 have 128 registers
 // each and spill (2560 x 16384 fp32 104 us, 96 with 512; 4660 x 9000 113 and 94).
 int lanes_per_row(int D, bool bf, bool back)

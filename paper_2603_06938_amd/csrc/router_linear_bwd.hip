@@ -1,5 +1,6 @@
 // Backward pass of the router's linear map:  du = dl W + du_add,  dW = dl^T u   (dl: gradient of the logits).
-// Bound by memory up to some hundred experts in bf16, some sixty in fp32: u is read once, du written once.  Neither product
+// Bound by memory up to 64 experts in bf16, some 32 in fp32: u is read once (for every 64 experts; again from the cache, where its
+// blocks follow each other on one XCD), du written once.  Neither product
 // goes through LDS: a wave owns 128 columns, eight consecutive ones to a lane, and column n of tile i is feature 8 n + i, so
 // that operands come as whole pieces of rows and a lane's results are consecutive features as well.  A bf16 matrix
 // instruction wants eight rows of one column in a lane: 8 x 8 elements are transposed in registers.
@@ -7,7 +8,8 @@
 //       waves are joined in LDS, those of the blocks by a second launch
 //   du  k runs over the experts: W is kept in registers, 16 tokens at a time
 // 16384 x 768 x 8 bf16 with both products (51 MB) 14.5 us, 4.1 of them the second launch; 32768 x 2048 x 64 with du_add (407 MB)
-// 95.8 us, 4.25 TB/s; 16384 x 2048 x 256 82.7 us, 415 TFLOP/s; 16384 x 2048 x 128 fp32 175 us, 98 of 154 TFLOP/s.
+// 95.8 us, 4.25 TB/s; 16384 x 2048 x 256 82.7 us, 415 TFLOP/s: neither memory nor matrix units (busy 18 %) bound it there, two waves
+// to a SIMD wait for loads, without registers for du's next step; 16384 x 2048 x 128 fp32 175 us, 98 of 154 TFLOP/s.
 #include "rows.hpp"
 
 namespace swimba {

@@ -5,8 +5,11 @@
 // A token lies in G lanes, in pieces of eight consecutive experts: 16 bytes of a bf16 row, so that a wave's loads are contiguous
 // where the experts fill the lanes.
 // Few experts are bound by memory and by their launches (2 x 16384 x 16 with padding 11.2 us, its gradient 4.8); many by what
-// the vector units have to issue: of the 30 us of 131072 x 256 top-8 in bf16 (75 MB, 12 us at the rate of a copy) they are busy
-// nine tenths, half of it with the picks.  The gradient is bound by memory (65536 x 256 fp32 29.5 us, 4.7 TB/s).
+// the vector units have to issue: of the 30 us of 131072 x 256 top-8 in bf16 (75 MB, 13 us for a kernel that only moves them) they
+// are busy nine tenths, half of it with the picks.  In fp32 more than 64 experts take 231 to 240 registers: two waves to a SIMD
+// (65536 x 256 27 us, the units busy six tenths).  65 to 255 experts in bf16 and 33 to 63 in fp32 spill 2 to 6 registers.
+// The gradient is bound by memory in fp32 (65536 x 256 29.5 us, 4.7 TB/s); in bf16, with twice the tokens for the bytes, the vector units
+// are busy three quarters of the time (131072 x 256 37 us, 26 for the bytes alone).
 #include "rows.hpp"
 
 namespace swimba {
@@ -399,7 +402,8 @@ int routing_lanes_of(int E) { return lanes_of(E) / pieces_of(E); }
 
 // Threads of a block and slices of a group.  A group that a block walks in one step, or in two with eight experts to a lane, stays
 // with it, without a second launch (8.7 us with 64 tokens of 256 experts top-8 in a step; with 512 in four steps 26.3, in two
-// launches 13).  Beyond, a slice is a step or more, and the slices of all groups are no more than the compute units: a block of
+// launches 13).  So does each of more than 128 groups, of which two slices would be more than the compute units: 129 groups of 2048 x 16
+// 11.3 us, 128 in two launches 13.5; of 2048 x 256, though, 100 and 57, until 255 groups fill the chip (103).  Beyond, a slice is a step or more, and the slices of all groups are no more than the compute units: a block of
 // 1024 threads fills one, and a 257th would run by itself (131072 x 256: 53.0 us with 257, 35.6 with 256).  Smaller blocks where
 // they are enough for that.
 struct Slices { int threads; int64_t count; };
