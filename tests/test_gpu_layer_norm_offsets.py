@@ -65,3 +65,23 @@ def test_large_offsets(D, io, res):
     du = torch.randn(T, D, generator=gen).to(IO[io]).to("cuda:0")
     back = sw.swimba_layer_norm_bwd(du[:16], r[:16], gamma, out.mean[:16], out.rstd[:16])
     assert (back.dgamma == 0).all()
+
+
+@pytest.mark.parametrize("D,io", [(1025, "f32"), (1030, "bf16"), (33, "f32")])
+def test_more_rows_than_blocks(D, io):
+    """2^20 blocks at most: beyond that many rows (times 16, of narrow ones) a block takes another."""
+    T = (1 << 20) * (16 if D <= 64 else 1) + 301
+    gen = torch.Generator("cuda:0").manual_seed(D)
+    x = torch.empty(T, D, dtype=IO[io], device="cuda:0")
+    x[:302] = torch.randn(302, D, device="cuda:0", generator=gen) + 100
+    x[302:-302] = 1.0
+    x[-302:] = torch.randn(302, D, device="cuda:0", generator=gen) - 50
+    gamma, beta = torch.randn(D, device="cuda:0", generator=gen), torch.randn(D, device="cuda:0", generator=gen)
+    out = sw.swimba_layer_norm(x, gamma, beta, 1e-5, want_stats=True)
+    for part in (slice(0, 302), slice(T - 302, T)):
+        rows = x[part].clone()
+        alone = sw.swimba_layer_norm(rows, gamma, beta, 1e-5, want_stats=True)
+        assert torch.equal(out.u[part], alone.u) and torch.equal(out.mean[part], alone.mean) and torch.equal(out.rstd[part], alone.rstd)
+        (u, m, s), (bu, bm, bs) = bounds(rows, 1e-5, gamma, beta)
+        check(alone.u, u, bu + half(rows.dtype) * (u.abs() + bu), "u")
+    assert (out.u[302:-302] == beta.to(x.dtype)).all()
