@@ -81,7 +81,8 @@ norm_fwd_kernel(const T *x, const R *residual, const float *__restrict__ gamma, 
     // What a mean is off by shifts every deviation, and its square goes into the variance.  Rows of bf16 are summed in 32 bits:
     // equal elements exactly (8 bits each, at most 2^14 of them), others to some 2^-18 of the largest, where each is stored to 2^-9.
     // Rows of fp32 are summed in 64, and what the mean loses in 32 bits is taken off the deviations as well; in 32 bits a row of
-    // 1000 times 12345.678 would come out at 0.5 instead of 0 (no slower: 16384 x 1024 22.8 us, 16384 x 4096 96; 4096 x 16384 120, 118 in 32 bits).
+    // 1000 times 12345.678 would come out at 0.5 instead of 0.  64 bits and 32: 16384 x 1024 22.8 us both, 16384 x 4096 96.5 and
+    // 99.8, 4096 x 16384 119.4 and 118.5, 262144 x 64 23.4 and 23.2.
     constexpr bool WIDE = sizeof(R) == 4;
     __shared__ float lds[2][1][16];
     __shared__ double lds64[2][16];

@@ -403,7 +403,8 @@ int routing_lanes_of(int E) { return lanes_of(E) / pieces_of(E); }
 // Threads of a block and slices of a group.  A group that a block walks in one step, or in two with eight experts to a lane, stays
 // with it, without a second launch (8.7 us with 64 tokens of 256 experts top-8 in a step; with 512 in four steps 26.3, in two
 // launches 13).  So does each of more than 128 groups, of which two slices would be more than the compute units: 129 groups of 2048 x 16
-// 11.3 us, 128 in two launches 13.5; of 2048 x 256, though, 100 and 57, until 255 groups fill the chip (103).  Beyond, a slice is a step or more, and the slices of all groups are no more than the compute units: a block of
+// 11.3 us, 128 in two launches 13.5; of 2048 x 256, though, 100 and 57, until 255 groups fill the chip (103).
+// In all other cases a slice is a step or more, and the slices of all groups are no more than the compute units: a block of
 // 1024 threads fills one, and a 257th would run by itself (131072 x 256: 53.0 us with 257, 35.6 with 256).  Smaller blocks where
 // they are enough for that.
 struct Slices { int threads; int64_t count; };
